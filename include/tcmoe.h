@@ -300,6 +300,52 @@ int moe_layer_fp8_host(const moe_shape_t* shape, const void* x_host, void* x_dev
                        const void* w3q, const float* s3, const void* w2q, const float* s2, void* y_dev, void* y_host,
                        void* ws, size_t ws_bytes, void* stream);
 
+/* ---- norm of the residual stream ---------------------------------------------------------------
+ * The step in front of the layer in a transformer block (Sec. II-A: the MoE layer reads the hidden states): the residual's
+ * addition, a root-mean-square norm and, for FP8 experts, the quantisation of its output, in one pass.  Per row of `cols` values:
+ *     s = x + residual (fp32);  rstd = 1 / sqrt(mean(s^2) + eps);  y = (s * weight) * rstd
+ *     scale = max|y| / 448 (1 where that is 0);  yq = e4m3(y / scale), round to nearest even, saturating
+ * y and yq are rounded once each, from the fp32 value.  yq / scale are what moe_expert_ffn_fp8 takes as xq / sx.
+ *   x, residual [rows, cols] bf16 (residual may be NULL: s = x);  weight [cols] bf16, or fp32 with weight_f32 != 0
+ *   res_out     NULL, or bf16 out: s (needs residual);  y NULL, or bf16 out;  yq, scale both NULL, or E4M3 codes [rows, cols] and fp32 [rows]
+ *   rstd        NULL, or fp32 [rows] out, for moe_rmsnorm_backward.  At least one of y and yq is not NULL.
+ * res_out and y may be x or residual themselves (not both the same buffer).  A row that holds a NaN or an infinity gives NaN; eps = 0 gives
+ * NaN for a row of zeros.  Limits: cols % 8 == 0, cols <= 16384 (MOE_ERR_UNSUPPORTED_SHAPE); eps >= 0.  Alignment: 16 bytes, yq 8, scale
+ * and rstd 4.  rows = 0 is accepted.  No workspace. */
+int moe_rmsnorm(const void* x, const void* residual, const void* weight, int32_t weight_f32, float eps, int64_t rows, int64_t cols,
+                void* res_out, void* y, void* yq, float* scale, float* rstd, void* stream);
+
+/* Gradients of moe_rmsnorm.  With s (the normed stream: res_out, or x where there was no residual), rstd as written by moe_rmsnorm, g = dy *
+ * weight and xhat = s * rstd:
+ *     dx = rstd * (g - xhat * mean(g * xhat)) + dres          bf16 [rows, cols]: the gradient of x and of residual alike
+ *     dweight = sum over the rows of dy * xhat                fp32 [cols], written whole (zeros for rows = 0)
+ * dres (NULL, or bf16 [rows, cols]) is the gradient that reaches s past the norm, through the skip path.  dx may be dy, dres or s.
+ * fp32 arithmetic, no atomics: the same bits every time.  ws: moe_rmsnorm_backward_workspace_bytes(rows, cols) bytes, 16-byte aligned, used
+ * during the call only (it need not be zeroed and has no status block).  Limits and alignment as moe_rmsnorm, rows < 2^31. */
+int moe_rmsnorm_backward_workspace_bytes(int64_t rows, int64_t cols, size_t* bytes);
+int moe_rmsnorm_backward(const void* dy, const void* dres, const void* s, const void* weight, int32_t weight_f32, const float* rstd,
+                         int64_t rows, int64_t cols, void* dx, float* dweight, void* ws, size_t ws_bytes, void* stream);
+
+/* ---- FP4 form of the expert FFN ------------------------------------------------------------------
+ * Microscaled 4-bit floating point (OCP Microscaling Formats 1.0, MXFP4): blocks of 32 neighbouring values of K share a power of two, held
+ * as one byte (E8M0): exponent ex = clamp(floor(log2(max|v|)) - 2, -127, 125), byte ex + 127; 127 for a block of zeros; 255 (NaN) for
+ * a block with a value that is not finite, all of which then reads as NaN.  Elements are E2M1 codes (sign, 0 0.5 1 1.5 2 3 4 6) of v / 2^ex,
+ * round to nearest even, saturating; two per byte, the lower index in the low half. */
+
+/* src bf16 [rows, cols] -> dst codes [rows, cols / 2] (bytes), scale bytes [rows, cols / 32], and back (the values are exact in bf16).
+ * cols % 32 == 0 (MOE_ERR_UNSUPPORTED_SHAPE).  bf16 rows 16-byte, codes 4-byte aligned. */
+int moe_quantize_rows_fp4(const void* src, int64_t rows, int64_t cols, void* dst, void* scale, void* stream);
+int moe_dequantize_rows_fp4(const void* src, const void* scale, int64_t rows, int64_t cols, void* dst, void* stream);
+
+/* w bf16 [E, K, N] (N contiguous, as moe_expert_ffn takes it) -> codes [E, N, K / 2] and the scales in the layout of the tensor cores, and
+ * back to bf16 [E, K, N].  The scale of block kb (of 32 along K) of column n of expert e is byte
+ *     ((e * ceil(N / 128) + n / 128) * 2 * ceil(K / 256) + kb / 4) * 512 + (n % 32) * 16 + (n % 128) / 32 * 4 + kb % 4
+ * of moe_fp4_scale_bytes(E, K, N) bytes; bytes that belong to no block hold 127 (the product relies on those past K).  K % 32 == 0, N % 8 == 0
+ * (MOE_ERR_UNSUPPORTED_SHAPE), E <= 65535.  Alignment: 16 bytes. */
+int moe_fp4_scale_bytes(int32_t E, int32_t K, int32_t N, size_t* bytes);
+int moe_quantize_weights_fp4(const void* w, int32_t E, int32_t K, int32_t N, void* wq, void* scale, void* stream);
+int moe_dequantize_weights_fp4(const void* wq, const void* scale, int32_t E, int32_t K, int32_t N, void* w, void* stream);
+
 /* Dispatch without a workspace (the paper has no counterpart; this entry point exists for
  * callers that cannot supply scratch memory).  Some users of this library run where device
  * memory cannot be obtained around the call: plugins that execute inside a host framework's

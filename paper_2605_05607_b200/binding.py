@@ -46,7 +46,9 @@ EXPORTS = ("moe_workspace_bytes", "moe_workspace_layout", "moe_status_reset", "m
            "moe_profile_enable", "moe_profile_read", "moe_dispatch_noalloc", "moe_quantize_rows",
            "moe_quantize_weights", "moe_expert_ffn_fp8", "moe_layer_fp8", "moe_layer_fp8_host", "moe_selftest_wait_timeout", "moe_traffic_stats", "moe_ep_pack", "moe_ep_finish",
            "moe_payload_efficiency", "moe_backward_workspace_bytes", "moe_layer_backward", "moe_clear_cache", "moe_gate_backward",
-           "moe_launch_count")
+           "moe_launch_count", "moe_rmsnorm", "moe_rmsnorm_backward_workspace_bytes", "moe_rmsnorm_backward",
+           "moe_quantize_rows_fp4", "moe_dequantize_rows_fp4", "moe_fp4_scale_bytes", "moe_quantize_weights_fp4",
+           "moe_dequantize_weights_fp4")
 
 
 class MoEShape(ctypes.Structure):
@@ -104,6 +106,15 @@ def lib() -> ctypes.CDLL:
         L.moe_gate_backward.argtypes = [shp, vp, vp, i64, vp, vp, lay, vp, vp, vp, vp, sz, vp]
         L.moe_ep_pack.argtypes = [shp, vp, vp, lay, vp, vp, vp]
         L.moe_ep_finish.argtypes = [shp, vp, lay, vp, vp]
+        i32 = ctypes.c_int32
+        L.moe_rmsnorm.argtypes = [vp, vp, vp, i32, ctypes.c_float, i64, i64, vp, vp, vp, vp, vp, vp]
+        L.moe_rmsnorm_backward_workspace_bytes.argtypes = [i64, i64, ctypes.POINTER(sz)]
+        L.moe_rmsnorm_backward.argtypes = [vp, vp, vp, vp, i32, vp, i64, i64, vp, vp, vp, sz, vp]
+        L.moe_quantize_rows_fp4.argtypes = [vp, i64, i64, vp, vp, vp]
+        L.moe_dequantize_rows_fp4.argtypes = [vp, vp, i64, i64, vp, vp]
+        L.moe_fp4_scale_bytes.argtypes = [i32, i32, i32, ctypes.POINTER(sz)]
+        L.moe_quantize_weights_fp4.argtypes = [vp, i32, i32, i32, vp, vp, vp]
+        L.moe_dequantize_weights_fp4.argtypes = [vp, vp, i32, i32, i32, vp, vp]
         L.moe_profile_enable.argtypes = [ctypes.c_int]
         L.moe_profile_read.argtypes = [ctypes.POINTER(ctypes.c_float), ctypes.POINTER(ctypes.c_int32)]
         L.moe_launch_count.argtypes = [ctypes.POINTER(i64)]
@@ -123,6 +134,12 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
         return None
     assert t.is_contiguous(), "tensors passed to the C ABI must be contiguous"
     return t.data_ptr()
+
+
+def _f32(t: Optional[torch.Tensor]) -> int:
+    """1 for fp32, 0 for bf16: the element type of a tensor that may be either."""
+    assert t is None or t.dtype in (torch.float32, torch.bfloat16), "bf16 or fp32"
+    return int(t is not None and t.dtype == torch.float32)
 
 
 def _stream(stream) -> Optional[int]:
@@ -261,6 +278,61 @@ def moe_layer_fp8_host(shape, x_host, x_dev, w_gate, logit_bias, w1q, s1, w3q, s
                                                           _ptr(logit_bias), stride, _ptr(w1q), _ptr(s1), _ptr(w3q),
                                                           _ptr(s3), _ptr(w2q), _ptr(s2), _ptr(y_dev), _ptr(y_host),
                                                           _ptr(ws), ws.numel(), _stream(stream)))
+
+
+def moe_rmsnorm(x, weight, eps: float, y=None, residual=None, res_out=None, yq=None, scale=None, rstd=None, stream=None) -> None:
+    """Root-mean-square norm of x (+ residual) per row: y bf16 and / or yq uint8 (E4M3 codes) with scale fp32 [rows].
+    weight bf16 or fp32; res_out bf16 takes the sum, rstd fp32 [rows] what the backward pass needs."""
+    rows, cols = x.shape
+    _check("moe_rmsnorm", lib().moe_rmsnorm(_ptr(x), _ptr(residual), _ptr(weight), _f32(weight), eps, rows, cols, _ptr(res_out),
+                                            _ptr(y), _ptr(yq), _ptr(scale), _ptr(rstd), _stream(stream)))
+
+
+def moe_rmsnorm_backward_workspace_bytes(rows: int, cols: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check("moe_rmsnorm_backward_workspace_bytes",
+           lib().moe_rmsnorm_backward_workspace_bytes(rows, cols, ctypes.byref(out)))
+    return out.value
+
+
+def moe_rmsnorm_backward(dy, s, weight, rstd, dx, dweight, ws, dres=None, stream=None) -> None:
+    """Gradients of moe_rmsnorm: s is the normed stream (res_out, or x without a residual), dres the skip path's gradient of it."""
+    rows, cols = dy.shape
+    _check("moe_rmsnorm_backward",
+           lib().moe_rmsnorm_backward(_ptr(dy), _ptr(dres), _ptr(s), _ptr(weight), _f32(weight), _ptr(rstd), rows, cols, _ptr(dx),
+                                      _ptr(dweight), _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream)))
+
+
+def moe_quantize_rows_fp4(src, dst, scale, stream=None) -> None:
+    """src bf16 [rows, cols] -> dst uint8 [rows, cols / 2] (E2M1 codes, two per byte), scale uint8 [rows, cols / 32] (E8M0)."""
+    rows, cols = src.shape
+    _check("moe_quantize_rows_fp4", lib().moe_quantize_rows_fp4(_ptr(src), rows, cols, _ptr(dst), _ptr(scale), _stream(stream)))
+
+
+def moe_dequantize_rows_fp4(src, scale, dst, stream=None) -> None:
+    """The inverse of moe_quantize_rows_fp4: dst bf16 [rows, cols]."""
+    rows, cols = dst.shape
+    _check("moe_dequantize_rows_fp4", lib().moe_dequantize_rows_fp4(_ptr(src), _ptr(scale), rows, cols, _ptr(dst), _stream(stream)))
+
+
+def moe_fp4_scale_bytes(E: int, K: int, N: int) -> int:
+    """Bytes of the scales that moe_quantize_weights_fp4 writes for weights [E, K, N]."""
+    out = ctypes.c_size_t(0)
+    _check("moe_fp4_scale_bytes", lib().moe_fp4_scale_bytes(E, K, N, ctypes.byref(out)))
+    return out.value
+
+
+def moe_quantize_weights_fp4(w, wq, scale, stream=None) -> None:
+    """w bf16 [E, K, N] -> wq uint8 [E, N, K / 2] (E2M1 codes, K contiguous), scale uint8, moe_fp4_scale_bytes(E, K, N) of them."""
+    E, K, N = w.shape
+    _check("moe_quantize_weights_fp4", lib().moe_quantize_weights_fp4(_ptr(w), E, K, N, _ptr(wq), _ptr(scale), _stream(stream)))
+
+
+def moe_dequantize_weights_fp4(wq, scale, w, stream=None) -> None:
+    """The inverse of moe_quantize_weights_fp4: w bf16 [E, K, N]."""
+    E, K, N = w.shape
+    _check("moe_dequantize_weights_fp4",
+           lib().moe_dequantize_weights_fp4(_ptr(wq), _ptr(scale), E, K, N, _ptr(w), _stream(stream)))
 
 
 def moe_ep_pack(shape, topk_idx, topk_w, layout: Layout, send_idx, send_w, stream=None) -> None:

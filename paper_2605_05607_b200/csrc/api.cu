@@ -634,6 +634,109 @@ int moe_quantize_weights(const void* w, int32_t E, int32_t K, int32_t N, void* w
   return MOE_OK;
 }
 
+namespace tcmoe {
+namespace {
+int check_norm(const void* weight, int64_t rows, int64_t cols) {
+  if (rows < 0 || cols <= 0 || weight == nullptr) return MOE_ERR_INVALID_ARG;
+  if (cols % 8 != 0 || cols > NORM_COLS || rows >= (1ll << 40)) return MOE_ERR_UNSUPPORTED_SHAPE;
+  return aligned(weight, 16) ? MOE_OK : MOE_ERR_MISALIGNED;
+}
+int check_rows_fp4(const void* rows_bf16, const void* codes, const void* scale, int64_t rows, int64_t cols) {
+  if (rows < 0 || cols <= 0 || cols > (1ll << 30)) return MOE_ERR_INVALID_ARG;
+  if (cols % 32 != 0 || rows >= (1ll << 32)) return MOE_ERR_UNSUPPORTED_SHAPE;
+  if (rows > 0 && (rows_bf16 == nullptr || codes == nullptr || scale == nullptr)) return MOE_ERR_INVALID_ARG;
+  return aligned(rows_bf16, 16) && aligned(codes, 4) ? MOE_OK : MOE_ERR_MISALIGNED;
+}
+int check_weights_fp4(const void* w, const void* wq, const void* scale, int32_t E, int32_t K, int32_t N) {
+  if (E <= 0 || K <= 0 || N <= 0 || E > 65535) return MOE_ERR_INVALID_ARG;
+  if (K % 32 != 0 || N % 8 != 0 || K > 65535 * 256) return MOE_ERR_UNSUPPORTED_SHAPE;
+  if (w == nullptr || wq == nullptr || scale == nullptr) return MOE_ERR_INVALID_ARG;
+  return aligned(w, 16) && aligned(wq, 16) && aligned(scale, 16) ? MOE_OK : MOE_ERR_MISALIGNED;
+}
+}  // namespace
+}  // namespace tcmoe
+
+int moe_rmsnorm(const void* x, const void* residual, const void* weight, int32_t weight_f32, float eps, int64_t rows, int64_t cols,
+                void* res_out, void* y, void* yq, float* scale, float* rstd, void* stream) {
+  int rc = check_norm(weight, rows, cols);
+  if (rc != MOE_OK) return rc;
+  if (!(eps >= 0.f) || eps > 3.0e38f) return MOE_ERR_INVALID_ARG;   // also refuses a NaN
+  if (rows > 0) {   // an empty tensor may have no address
+    if (x == nullptr || (yq == nullptr) != (scale == nullptr) || (y == nullptr && yq == nullptr)) return MOE_ERR_INVALID_ARG;
+    if (res_out != nullptr && (residual == nullptr || res_out == y)) return MOE_ERR_INVALID_ARG;
+  }
+  if (!aligned(x, 16) || !aligned(residual, 16) || !aligned(res_out, 16) || !aligned(y, 16) || !aligned(yq, 8) || !aligned(scale, 4) ||
+      !aligned(rstd, 4))
+    return MOE_ERR_MISALIGNED;
+  if (!have_device()) return MOE_ERR_CUDA;
+  TCMOE_CUDA(launch_rmsnorm(x, residual, weight, weight_f32 != 0, eps, rows, (int)cols, res_out, y, yq, scale, rstd,
+                            static_cast<cudaStream_t>(stream)));
+  return MOE_OK;
+}
+
+int moe_rmsnorm_backward_workspace_bytes(int64_t rows, int64_t cols, size_t* bytes) {
+  if (rows < 0 || cols <= 0 || bytes == nullptr) return MOE_ERR_INVALID_ARG;
+  if (cols % 8 != 0 || cols > NORM_COLS || rows >= (1ll << 31)) return MOE_ERR_UNSUPPORTED_SHAPE;
+  *bytes = round_up((size_t)rmsnorm_parts(rows) * (size_t)cols * 4, ALIGN);
+  return MOE_OK;
+}
+
+int moe_rmsnorm_backward(const void* dy, const void* dres, const void* s, const void* weight, int32_t weight_f32, const float* rstd,
+                         int64_t rows, int64_t cols, void* dx, float* dweight, void* ws, size_t ws_bytes, void* stream) {
+  int rc = check_norm(weight, rows, cols);
+  if (rc != MOE_OK) return rc;
+  if (dweight == nullptr) return MOE_ERR_INVALID_ARG;
+  if (rows > 0 && (dy == nullptr || s == nullptr || rstd == nullptr || dx == nullptr || ws == nullptr)) return MOE_ERR_INVALID_ARG;
+  if (!aligned(dy, 16) || !aligned(dres, 16) || !aligned(s, 16) || !aligned(dx, 16) || !aligned(dweight, 16) || !aligned(ws, 16) ||
+      !aligned(rstd, 4))
+    return MOE_ERR_MISALIGNED;
+  size_t need = 0;
+  if ((rc = moe_rmsnorm_backward_workspace_bytes(rows, cols, &need)) != MOE_OK) return rc;
+  if (ws_bytes < need) return MOE_ERR_WORKSPACE_TOO_SMALL;
+  if (!have_device()) return MOE_ERR_CUDA;
+  TCMOE_CUDA(launch_rmsnorm_backward(dy, dres, s, weight, weight_f32 != 0, rstd, rows, (int)cols, dx, dweight, static_cast<float*>(ws),
+                                     static_cast<cudaStream_t>(stream)));
+  return MOE_OK;
+}
+
+int moe_quantize_rows_fp4(const void* src, int64_t rows, int64_t cols, void* dst, void* scale, void* stream) {
+  const int rc = check_rows_fp4(src, dst, scale, rows, cols);
+  if (rc != MOE_OK) return rc;
+  if (!have_device()) return MOE_ERR_CUDA;
+  TCMOE_CUDA(launch_quantize_rows_fp4(src, rows, (int)cols, dst, scale, static_cast<cudaStream_t>(stream)));
+  return MOE_OK;
+}
+
+int moe_dequantize_rows_fp4(const void* src, const void* scale, int64_t rows, int64_t cols, void* dst, void* stream) {
+  const int rc = check_rows_fp4(dst, src, scale, rows, cols);
+  if (rc != MOE_OK) return rc;
+  if (!have_device()) return MOE_ERR_CUDA;
+  TCMOE_CUDA(launch_dequantize_rows_fp4(src, scale, rows, (int)cols, dst, static_cast<cudaStream_t>(stream)));
+  return MOE_OK;
+}
+
+int moe_fp4_scale_bytes(int32_t E, int32_t K, int32_t N, size_t* bytes) {
+  if (E <= 0 || K <= 0 || N <= 0 || E > 65535 || bytes == nullptr) return MOE_ERR_INVALID_ARG;
+  *bytes = fp4_scale_bytes((size_t)E * (((size_t)N + 127) / 128), K);
+  return MOE_OK;
+}
+
+int moe_quantize_weights_fp4(const void* w, int32_t E, int32_t K, int32_t N, void* wq, void* scale, void* stream) {
+  const int rc = check_weights_fp4(w, wq, scale, E, K, N);
+  if (rc != MOE_OK) return rc;
+  if (!have_device()) return MOE_ERR_CUDA;
+  TCMOE_CUDA(launch_quantize_weights_fp4(w, E, K, N, wq, scale, static_cast<cudaStream_t>(stream)));
+  return MOE_OK;
+}
+
+int moe_dequantize_weights_fp4(const void* wq, const void* scale, int32_t E, int32_t K, int32_t N, void* w, void* stream) {
+  const int rc = check_weights_fp4(w, wq, scale, E, K, N);
+  if (rc != MOE_OK) return rc;
+  if (!have_device()) return MOE_ERR_CUDA;
+  TCMOE_CUDA(launch_dequantize_weights_fp4(wq, scale, E, K, N, w, static_cast<cudaStream_t>(stream)));
+  return MOE_OK;
+}
+
 int moe_expert_ffn_fp8(const moe_shape_t* shape, const void* xq, const float* sx, const moe_layout_t* layout,
                        const float* topk_w, const void* w1q, const float* s1, const void* w3q, const float* s3,
                        const void* w2q, const float* s2, void* o, void* ws, size_t ws_bytes, void* stream) {

@@ -250,6 +250,21 @@ cudaError_t launch_ep_finish(const Shape& s, const void* back, const Layout& L, 
 // quant.cu: bf16 -> E4M3 with one scale per row / per (expert, output column)
 cudaError_t launch_quantize_rows(const void* src, long long rows, int cols, void* dst, float* scale, cudaStream_t st);
 cudaError_t launch_quantize_weights(const void* w, int E, int K, int N, void* wq, float* scale, cudaStream_t st);
+// norm.cu: root-mean-square norm of the residual stream in front of the layer, and its backward pass
+constexpr int NORM_COLS = 16384;  // columns at most
+constexpr int NORM_PARTS = 592;   // blocks that add up the weight gradient, at most (four per SM)
+int rmsnorm_parts(long long rows);
+cudaError_t launch_rmsnorm(const void* x, const void* res, const void* w, bool w32, float eps, long long rows, int cols, void* res_out,
+                           void* y, void* yq, float* scale, float* rstd, cudaStream_t st);
+cudaError_t launch_rmsnorm_backward(const void* dy, const void* dres, const void* s, const void* w, bool w32, const float* rstd,
+                                    long long rows, int cols, void* dx, float* dw, float* part, cudaStream_t st);
+// quant4.cu: bf16 <-> E2M1 with a power of two per 32 values
+// bytes of scale chunks for `tiles` tiles of 128 rows (columns) over K
+inline size_t fp4_scale_bytes(size_t tiles, int K) { return tiles * (((size_t)K + 255) / 256) * 1024; }
+cudaError_t launch_quantize_rows_fp4(const void* src, long long rows, int cols, void* dst, void* scale, cudaStream_t st);
+cudaError_t launch_dequantize_rows_fp4(const void* src, const void* scale, long long rows, int cols, void* dst, cudaStream_t st);
+cudaError_t launch_quantize_weights_fp4(const void* w, int E, int K, int N, void* wq, void* scale, cudaStream_t st);
+cudaError_t launch_dequantize_weights_fp4(const void* wq, const void* scale, int E, int K, int N, void* w, cudaStream_t st);
 int sm_count();
 int current_device();   // index of the current CUDA device, clamped to [0, MAX_DEVICES)
 constexpr int MAX_DEVICES = 64;   // per-device caches (kernel attributes, SM counts) are arrays of this size

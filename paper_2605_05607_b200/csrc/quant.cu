@@ -4,35 +4,11 @@
 //           (weights); 1 for an all-zero vector
 //   code  = e4m3(fl32(v / scale)), round to nearest even, saturating at +-448
 // Every step is a single fp32 operation, so a CPU restatement takes the same decisions.
-#include "common.cuh"
-
-#include <cuda_bf16.h>
-#include <cuda_fp8.h>
+#include "quant.cuh"
 
 namespace tcmoe {
 namespace {
 
-__device__ __forceinline__ uint8_t to_e4m3(float v, float scale) {
-  return (uint8_t)__nv_cvt_float_to_fp8(__fdiv_rn(v, scale), __NV_SATFINITE, __NV_E4M3);
-}
-__device__ __forceinline__ float scale_of(float amax) { return amax == 0.f ? 1.f : __fdiv_rn(amax, 448.f); }
-
-// Two codes at once, the low byte that of `a`.  fl32(v / scale) comes from the reciprocal, which the whole row shares, by
-// Markstein's correction (P. Markstein, "Computation of elementary functions on the IBM RISC System/6000 processor", IBM J. Res.
-// Dev. 34, 1990): with inv = RN(1 / s) and q within an ulp of v / s, RN(q + (v - q s) * inv), the residual exact, is RN(v / s) as long
-// as nothing leaves the normal range.  Values so small that the residual does round to code 0 either way.  (Taking the code
-// where both ends of an error interval around v * inv agree was no faster than dividing: quotients of 8-bit significands
-// tie exactly too often, and one lane's division stops its warp.)
-__device__ __forceinline__ uint32_t to_e4m3_pair(float a, float b, float inv, float scale) {
-  float qa = a * inv, qb = b * inv;
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {   // the first step makes q faithful, the second is the one that rounds correctly
-    qa = fmaf(fmaf(-qa, scale, a), inv, qa);
-    qb = fmaf(fmaf(-qb, scale, b), inv, qb);
-  }
-  return __nv_cvt_float2_to_fp8x2(make_float2(copysignf(qa, a), copysignf(qb, b)),   // -0 stays -0
-                                  __NV_SATFINITE, __NV_E4M3);
-}
 // WARPS warps per row (1, or the whole block of 4 for long rows; up to 2048 columns many rows take one warp each, few the block).  The row stays in registers between the maximum and the codes
 // when it has at most KEEP vectors per lane; a longer one is read again.  cols % 8 == 0.  Bound by memory now, by the divisions
 // before: 131072 rows of 1536 columns 152 -> 101 us (6.0 TB/s), 131072 of 4096 370 -> 281 (5.7 TB/s), 16384 of 4096, which stay in L2, 64 -> 37.
@@ -76,7 +52,7 @@ __global__ void __launch_bounds__(WARPS == 1 ? 256 : WARPS * 32) quantize_rows_k
     const float sc = scale_of(amax);
     if (lane == 0) scale[r] = sc;
     uint2* out = dst + r * vec_per_row;
-    if (!(sc >= 0x1p-80f && sc < 0x1p100f)) {   // the reciprocal or a residual could leave the normal range: divide
+    if (!e4m3_pair_exact(sc)) {   // the reciprocal or a residual could leave the normal range: divide
 #pragma unroll 1
       for (int v = lane; v < vec_per_row; v += LANES) {
         const uint4 raw = __ldg(row + v);

@@ -1,0 +1,231 @@
+"""The norm of the residual stream and its gradients against float64, through the C ABI."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import norm_oracle as N
+from paper_2605_05607_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+
+U32, U16 = 2.0 ** -24, 2.0 ** -8      # half a step of fp32 and of bf16, relative
+EPS = 1e-6
+# fp32 roundings on the longest way to a row's sum: 64 terms per thread, 5 + 16 partial sums, and one each for s, its square, the mean, eps
+# and the root (which halves what comes before it)
+CHAIN = 64 + 21 + 5
+
+
+def f64(t):
+    return t.double().cpu().numpy()
+
+
+def make(rows, cols, seed, res=True, w32=False):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    rnd = lambda *s: torch.randn(*s, generator=g, device="cuda")   # noqa: E731
+    x = rnd(rows, cols).bfloat16()
+    r = (rnd(rows, cols) * 3).bfloat16() if res else None
+    w = 1 + 0.3 * rnd(cols)
+    return x, r, (w if w32 else w.bfloat16())
+
+
+def e4m3(codes):
+    return f64(codes.view(torch.float8_e4m3fn).float())
+
+
+def check_forward(x, r, w, out, eps=EPS):
+    s, rstd, y = N.rmsnorm(f64(x), None if r is None else f64(r), f64(w), eps)
+    assert (np.abs(f64(out["rstd"]) - rstd) <= CHAIN * U32 * rstd).all()
+    y_err = (CHAIN + 4) * U32 * np.abs(y)
+    if "res" in out:
+        assert (np.abs(f64(out["res"]) - s) <= (U16 + U32) * np.abs(s)).all()
+    if "y" in out:
+        assert (np.abs(f64(out["y"]) - y) <= U16 * np.abs(y) + (1 + U16) * y_err).all()
+    if "q" in out:
+        top = np.abs(y).max(axis=1)
+        sc = f64(out["scale"])
+        ref = np.where(top == 0, 1.0, top / 448)
+        assert (np.abs(sc - ref) <= (CHAIN + 6) * U32 * ref).all()
+        # half a step of E4M3: 2^-4 of a normal value, 2^-10 of the scale below 2^-6
+        got = e4m3(out["q"]) * sc[:, None]
+        assert (np.abs(got - y) <= (2.0 ** -4 + 2.0 ** -18) * np.abs(y) + 2.0 ** -10 * sc[:, None]).all()
+
+
+def forward(x, r, w, y=True, q=True, eps=EPS, keep=True):
+    rows, cols = x.shape
+    out = {"rstd": torch.full((rows,), 7.0, device="cuda")}
+    if y:
+        out["y"] = torch.full_like(x, 7.0)
+    if q:
+        out["q"] = torch.full((rows, cols), 9, dtype=torch.uint8, device="cuda")
+        out["scale"] = torch.full((rows,), 7.0, device="cuda")
+    if r is not None and keep:
+        out["res"] = torch.full_like(x, 7.0)
+    B.moe_rmsnorm(x, w, eps, y=out.get("y"), residual=r, res_out=out.get("res"), yq=out.get("q"), scale=out.get("scale"),
+                  rstd=out["rstd"])
+    return out
+
+
+COLS = [8, 16, 248, 256, 264, 512, 520, 1024, 1032, 2048, 2056, 2880, 4096, 4104, 7168, 8192, 8200, 16384]
+
+
+@pytest.mark.parametrize("cols", COLS)
+@pytest.mark.parametrize("rows", [1, 7, 300])
+def test_norm_matches_float64(rows, cols):
+    for i, (res, y, q, w32) in enumerate([(True, True, True, False), (False, True, False, True), (True, False, True, True),
+                                          (False, False, True, False), (True, True, False, False), (False, True, True, True)]):
+        x, r, w = make(rows, cols, 100 * rows + cols + i, res, w32)
+        check_forward(x, r, w, forward(x, r, w, y, q))
+
+
+def test_norm_of_many_rows():
+    """More rows than blocks, so that each takes several."""
+    for cols in (64, 640, 1536, 4096):
+        x, r, w = make(9001, cols, cols)
+        check_forward(x, r, w, forward(x, r, w))
+
+
+def test_norm_in_place_and_without_the_optional_outputs():
+    x, r, w = make(50, 2880, 3)
+    want = forward(x, r, w)
+    stream, y = r.clone(), x.clone()
+    B.moe_rmsnorm(y, w, EPS, y=y, residual=stream, res_out=stream)          # y over x, the stream over itself
+    assert torch.equal(y, want["y"]) and torch.equal(stream, want["res"])
+    stream, y = x.clone(), r.clone()
+    B.moe_rmsnorm(stream, w, EPS, y=y, residual=y, res_out=stream)          # y over the residual, the sum over x
+    assert torch.equal(y, want["y"]) and torch.equal(stream, want["res"])
+    out = forward(x, r, w, keep=False)
+    assert torch.equal(out["y"], want["y"]) and torch.equal(out["q"], want["q"])
+
+
+def test_norm_rows_of_extreme_values():
+    cols = 512
+    x = torch.zeros(8, cols, device="cuda").bfloat16()
+    w = torch.ones(cols, device="cuda")
+    x[1] = 1e-20                       # vanishes against eps
+    x[2, 5] = 1e18                     # one huge value: everything else underflows
+    x[3] = 2.0 ** -133                 # the least subnormal
+    x[4, 0], x[5, 0], x[6, 0] = float("nan"), float("inf"), -float("inf")
+    x[7] = 3.0
+    out = forward(x, None, w)
+    keep = [0, 1, 2, 3, 7]
+    check_forward(x[keep], None, w, {n: t[keep] for n, t in out.items()})
+    assert (e4m3(out["q"])[0] == 0).all() and out["scale"][0].item() == 1.0
+    for row in (4, 5, 6):
+        assert torch.isnan(out["y"][row]).any() and torch.isnan(out["scale"][row])
+        assert np.isnan(e4m3(out["q"])[row]).all()
+    assert torch.isnan(out["y"][4]).all()
+    zero = forward(x[:1], None, w, eps=0.0)   # 0 / 0
+    assert torch.isnan(zero["y"]).all()
+    # values so small that the scale itself vanishes: codes of zero, not of infinity
+    tiny = forward(x[7:8], None, torch.full((cols,), 2.0 ** -148, device="cuda"))
+    assert tiny["scale"].item() == 1.0 and (e4m3(tiny["q"]) == 0).all()
+
+
+def test_norm_of_no_rows_and_untouched_neighbours():
+    w = torch.ones(256, device="cuda")
+    pad = torch.full((3, 256), 5.0, device="cuda").bfloat16()
+    B.moe_rmsnorm(pad[:0], w, EPS, y=pad[:0])
+    x, r, _ = make(5, 256, 1)
+    y, sc, rs = torch.full((7, 256), 5.0, device="cuda").bfloat16(), torch.full((7,), 5.0, device="cuda"), torch.full((7,), 5.0, device="cuda")
+    q = torch.full((7, 256), 5, dtype=torch.uint8, device="cuda")
+    B.moe_rmsnorm(x, w, EPS, y=y[1:6], residual=r, yq=q[1:6], scale=sc[1:6], rstd=rs[1:6])
+    torch.cuda.synchronize()
+    assert (pad == 5).all()
+    for t in (y, q, sc, rs):
+        assert (t[0] == 5).all() and (t[6] == 5).all() and not (t[1:6] == 5).all()
+
+
+def check_backward(dy, s, w, rstd, skip, dx, dw):
+    rows, cols = dy.shape
+    a, sv, wv, rv = f64(dy), f64(s), f64(w), f64(rstd)
+    k = None if skip is None else f64(skip)
+    dx_ref, dw_ref = N.rmsnorm_backward(a, sv, wv, rv, k)
+    xhat, g = sv * rv[:, None], a * wv
+    # every term of dx passes a handful of roundings, those of the mean up to CHAIN
+    mag = rv[:, None] * (6 * np.abs(g) + np.abs(xhat) * (CHAIN + 6) * np.abs(g * xhat).mean(axis=1, keepdims=True))
+    err = U32 * (mag + np.abs(dx_ref) + (0 if k is None else np.abs(k)))
+    assert (np.abs(f64(dx) - dx_ref) <= U16 * np.abs(dx_ref) + (1 + U16) * err).all()
+    # dw: additions in a row inside a block, then over a warp's share of the blocks, then over eight warps
+    depth = -(-rows // 592) + 592 // 8 + 8 + 4
+    assert (np.abs(f64(dw) - dw_ref) <= depth * U32 * np.abs(a * xhat).sum(axis=0) + 1e-300).all()
+
+
+def backward(dy, s, w, rstd, skip=None):
+    rows, cols = dy.shape
+    dx, dw = torch.full_like(dy, 7.0), torch.full((cols,), 7.0, device="cuda")
+    ws = torch.full((B.moe_rmsnorm_backward_workspace_bytes(rows, cols),), 255, dtype=torch.uint8, device="cuda")
+    B.moe_rmsnorm_backward(dy, s, w, rstd, dx, dw, ws, dres=skip)
+    return dx, dw
+
+
+@pytest.mark.parametrize("cols", COLS)
+@pytest.mark.parametrize("rows", [1, 5, 700])
+def test_norm_backward_matches_float64(rows, cols):
+    for skip, w32 in ((True, False), (False, True)):
+        x, r, w = make(rows, cols, rows + cols, True, w32)
+        out = forward(x, r, w, q=False)
+        g = torch.Generator(device="cuda").manual_seed(rows)
+        dy = torch.randn(rows, cols, generator=g, device="cuda").bfloat16()
+        k = torch.randn(rows, cols, generator=g, device="cuda").bfloat16() if skip else None
+        check_backward(dy, out["res"], w, out["rstd"], k, *backward(dy, out["res"], w, out["rstd"], k))
+
+
+def test_norm_gradients_against_differences():
+    """Central differences of sum(c * y) in float64, at the kernel's own inputs."""
+    x, _, w = make(3, 40, 9, False, True)
+    rstd = forward(x, None, w, q=False)["rstd"]
+    c = torch.randn(3, 40, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").bfloat16()
+    dx, dw = backward(c, x, w, rstd)
+    X, W, C, h = f64(x), f64(w), f64(c), 1e-5
+    loss = lambda X, W: (C * N.rmsnorm(X, None, W, EPS)[2]).sum()   # noqa: E731
+    for i, j in ((0, 0), (1, 17), (2, 39)):
+        d = np.zeros_like(X)
+        d[i, j] = h
+        num = (loss(X + d, W) - loss(X - d, W)) / (2 * h)
+        assert abs(num - f64(dx)[i, j]) <= U16 * abs(num) + 2e-5      # bf16; differences are good to 1e-8, rstd to 6e-6
+    for j in (0, 39):
+        d = np.zeros_like(W)
+        d[j] = h
+        num = (loss(X, W + d) - loss(X, W - d)) / (2 * h)
+        assert abs(num - f64(dw)[j]) <= 2e-5 * max(1, abs(num))
+
+
+def test_norm_backward_in_place_of_no_rows_and_the_same_every_time():
+    x, r, w = make(333, 1000, 4)
+    out = forward(x, r, w, q=False)
+    dy, k = torch.randn_like(x), torch.randn_like(x)
+    dx, dw = backward(dy, out["res"], w, out["rstd"], k)
+    again = backward(dy, out["res"], w, out["rstd"], k)
+    assert torch.equal(dx, again[0]) and torch.equal(dw, again[1])
+    ws = torch.empty(B.moe_rmsnorm_backward_workspace_bytes(333, 1000), dtype=torch.uint8, device="cuda")
+    for which in range(3):                                   # dx over dy, over dres, over s
+        bufs = [dy.clone(), k.clone(), out["res"].clone()]
+        B.moe_rmsnorm_backward(bufs[0], bufs[2], w, out["rstd"], bufs[which], again[1], ws, dres=bufs[1])
+        assert torch.equal(bufs[which], dx) and torch.equal(again[1], dw)
+    dw.fill_(7)
+    B.moe_rmsnorm_backward(dy[:0], x[:0], w, out["rstd"][:0], dx[:0], dw, None)
+    assert (dw == 0).all()
+
+
+def test_norm_captured_and_on_another_stream():
+    x, r, w = make(64, 4096, 5)
+    want, dyw = forward(x, r, w), torch.randn_like(x)
+    bwd = backward(dyw, want["res"], w, want["rstd"])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    y, q, sc, rs, res = (torch.zeros_like(want[n]) for n in ("y", "q", "scale", "rstd", "res"))
+    dx, dw = torch.zeros_like(bwd[0]), torch.zeros_like(bwd[1])
+    ws = torch.empty(B.moe_rmsnorm_backward_workspace_bytes(64, 4096), dtype=torch.uint8, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    xs = x.clone()
+    with torch.cuda.graph(graph, stream=side):
+        B.moe_rmsnorm(xs, w, EPS, y=y, residual=r, res_out=res, yq=q, scale=sc, rstd=rs)
+        B.moe_rmsnorm_backward(dyw, res, w, rs, dx, dw, ws)
+    xs.zero_()
+    graph.replay()
+    xs.copy_(x)
+    graph.replay()
+    torch.cuda.synchronize()
+    for got, name in ((y, "y"), (q, "q"), (sc, "scale"), (rs, "rstd"), (res, "res")):
+        assert torch.equal(got, want[name]), name
+    assert torch.equal(dx, bwd[0]) and torch.equal(dw, bwd[1])
