@@ -346,6 +346,24 @@ int moe_fp4_scale_bytes(int32_t E, int32_t K, int32_t N, size_t* bytes);
 int moe_quantize_weights_fp4(const void* w, int32_t E, int32_t K, int32_t N, void* wq, void* scale, void* stream);
 int moe_dequantize_weights_fp4(const void* wq, const void* scale, int32_t E, int32_t K, int32_t N, void* w, void* stream);
 
+/* moe_expert_ffn on quantised operands: xq codes [rows of the dispatched buffer, d / 2] with scale bytes sx [rows, d / 32] (from
+ * moe_quantize_rows_fp4; row r of expert e reads dispatched row layout->row_src[r]); w1q, w3q [E, f, d / 2] and w2q [E, d, f / 2] with their
+ * scales, all from moe_quantize_weights_fp4.  Products of the codes and their scales accumulate in fp32;
+ *     h = silu(a W1) * (a W3) is quantised from fp32, by the rule above, in GEMM-1's epilogue;  o = w_r * (hq W2), bf16 [T*k, d]
+ * (gate weight w_r in the epilogue unless MOE_FLAG_WEIGHT_IN_COMBINE).  A NaN scale makes what it scales NaN.  Rows behind the last pair
+ * in use (MOE_FLAG_SPARSE_TOPK) are left as they were.  Needs d % 32 == 0 and f % 32 == 0 (MOE_ERR_UNSUPPORTED_SHAPE); of the flags only
+ * MOE_FLAG_WEIGHT_IN_COMBINE and MOE_FLAG_SPARSE_TOPK (MOE_ERR_INVALID_ARG).  Alignment: codes and o 128 bytes, weight scales 16, sx any. */
+int moe_expert_ffn_fp4(const moe_shape_t* shape, const void* xq, const void* sx, const moe_layout_t* layout, const float* topk_w,
+                       const void* w1q, const void* s1, const void* w3q, const void* s3, const void* w2q, const void* s2, void* o,
+                       void* ws, size_t ws_bytes, void* stream);
+
+/* moe_layer with FP4 experts: gate, top-k and layout on the bf16 activations as in moe_layer, x quantised into the workspace, the experts as
+ * in moe_expert_ffn_fp4, Combine as in moe_layer.  Optional outputs and limits as moe_layer, plus d % 32 == 0 and f % 32 == 0; of the
+ * flags MOE_FLAG_WEIGHT_IN_COMBINE only. */
+int moe_layer_fp4(const moe_shape_t* shape, const void* x, const float* w_gate, const float* logit_bias, int64_t bias_row_stride,
+                  const void* w1q, const void* s1, const void* w3q, const void* s3, const void* w2q, const void* s2, void* y,
+                  float* logits, int32_t* topk_idx, float* topk_w, const moe_layout_t* layout, void* ws, size_t ws_bytes, void* stream);
+
 /* Dispatch without a workspace (the paper has no counterpart; this entry point exists for
  * callers that cannot supply scratch memory).  Some users of this library run where device
  * memory cannot be obtained around the call: plugins that execute inside a host framework's

@@ -48,7 +48,7 @@ EXPORTS = ("moe_workspace_bytes", "moe_workspace_layout", "moe_status_reset", "m
            "moe_payload_efficiency", "moe_backward_workspace_bytes", "moe_layer_backward", "moe_clear_cache", "moe_gate_backward",
            "moe_launch_count", "moe_rmsnorm", "moe_rmsnorm_backward_workspace_bytes", "moe_rmsnorm_backward",
            "moe_quantize_rows_fp4", "moe_dequantize_rows_fp4", "moe_fp4_scale_bytes", "moe_quantize_weights_fp4",
-           "moe_dequantize_weights_fp4")
+           "moe_dequantize_weights_fp4", "moe_expert_ffn_fp4", "moe_layer_fp4")
 
 
 class MoEShape(ctypes.Structure):
@@ -115,6 +115,8 @@ def lib() -> ctypes.CDLL:
         L.moe_fp4_scale_bytes.argtypes = [i32, i32, i32, ctypes.POINTER(sz)]
         L.moe_quantize_weights_fp4.argtypes = [vp, i32, i32, i32, vp, vp, vp]
         L.moe_dequantize_weights_fp4.argtypes = [vp, vp, i32, i32, i32, vp, vp]
+        L.moe_expert_ffn_fp4.argtypes = [shp, vp, vp, lay, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.moe_layer_fp4.argtypes = L.moe_layer_fp8.argtypes
         L.moe_profile_enable.argtypes = [ctypes.c_int]
         L.moe_profile_read.argtypes = [ctypes.POINTER(ctypes.c_float), ctypes.POINTER(ctypes.c_int32)]
         L.moe_launch_count.argtypes = [ctypes.POINTER(i64)]
@@ -333,6 +335,25 @@ def moe_dequantize_weights_fp4(wq, scale, w, stream=None) -> None:
     E, K, N = w.shape
     _check("moe_dequantize_weights_fp4",
            lib().moe_dequantize_weights_fp4(_ptr(wq), _ptr(scale), E, K, N, _ptr(w), _stream(stream)))
+
+
+def moe_expert_ffn_fp4(shape, xq, sx, layout: Layout, topk_w, w1q, s1, w3q, s3, w2q, s2, o, ws, stream=None) -> None:
+    c = layout.c()
+    _check("moe_expert_ffn_fp4", lib().moe_expert_ffn_fp4(ctypes.byref(shape), _ptr(xq), _ptr(sx), ctypes.byref(c),
+                                                          _ptr(topk_w), _ptr(w1q), _ptr(s1), _ptr(w3q), _ptr(s3),
+                                                          _ptr(w2q), _ptr(s2), _ptr(o), _ptr(ws), ws.numel(),
+                                                          _stream(stream)))
+
+
+def moe_layer_fp4(shape, x, w_gate, logit_bias, w1q, s1, w3q, s3, w2q, s2, y, ws, logits=None, topk_idx=None,
+                  topk_w=None, layout: Optional[Layout] = None, stream=None) -> None:
+    stride = 0 if logit_bias is None or logit_bias.dim() == 1 else shape.E
+    c = layout.c() if layout is not None else None
+    _check("moe_layer_fp4", lib().moe_layer_fp4(ctypes.byref(shape), _ptr(x), _ptr(w_gate), _ptr(logit_bias), stride,
+                                                _ptr(w1q), _ptr(s1), _ptr(w3q), _ptr(s3), _ptr(w2q), _ptr(s2),
+                                                _ptr(y), _ptr(logits), _ptr(topk_idx), _ptr(topk_w),
+                                                ctypes.byref(c) if c is not None else None, _ptr(ws), ws.numel(),
+                                                _stream(stream)))
 
 
 def moe_ep_pack(shape, topk_idx, topk_w, layout: Layout, send_idx, send_w, stream=None) -> None:

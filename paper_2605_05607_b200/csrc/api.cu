@@ -19,7 +19,7 @@ inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 // Regions of the workspace, in order.  Every region starts on a 1 KiB boundary.
 struct WsPlan {
   size_t status, emask, gmask, eprefix, gprefix, mt_prefix, mp_prefix, blk_start, blk_info, n_blocks, tracker, wsplit, xs, h, hq, sh, xq, sx, o, logits, topk_idx, topk_w;
-  size_t expert_counts, expert_offsets, group_counts, group_offsets, pair_row, row_pair, al, disp_token, row_src;
+  size_t expert_counts, expert_offsets, group_counts, group_offsets, pair_row, row_pair, al, disp_token, row_src, sf_x, sf_h;
   size_t total;
   int W;
 };
@@ -90,6 +90,10 @@ WsPlan plan(const moe_shape_t& s) {
   p.al = take(G * T * 4);
   p.disp_token = take(T * kg * 4);
   p.row_src = take(P * 4);
+  // FP4 form: scale chunks of the row tiles of x and of h (the sorted codes of x lie in `o`, those of h in `h`)
+  const bool fp4 = s.d % 32 == 0 && s.f % 32 == 0;
+  p.sf_x = take(fp4 ? fp4_scale_bytes((size_t)fp4_row_tiles(to_shape(s)), s.d) : 0);
+  p.sf_h = take(fp4 ? fp4_scale_bytes((size_t)fp4_row_tiles(to_shape(s)), s.f) : 0);
   p.total = off;
   return p;
 }
@@ -789,6 +793,59 @@ int moe_expert_ffn_fp8(const moe_shape_t* shape, const void* xq, const float* sx
   return MOE_OK;
 }
 
+namespace tcmoe {
+namespace {
+// flags that name forms of the bf16 / FP8 products, or steps inside them
+constexpr int kNotFp4 = MOE_FLAG_FUSED_FFN | MOE_FLAG_SM_PARTITION | MOE_FLAG_TRACK_DISPATCH | MOE_FLAG_COMBINE_IN_EPILOGUE |
+                        MOE_FLAG_GEMM1_PAIR | MOE_FLAG_GEMM1_GATHER | MOE_FLAG_GEMM2_PAIR | MOE_FLAG_GEMM2_SINGLE;
+int check_fp4(const moe_shape_t* s, const void* w1q, const void* s1, const void* w3q, const void* s3, const void* w2q, const void* s2) {
+  if (s->d % 32 != 0 || s->f % 32 != 0) return MOE_ERR_UNSUPPORTED_SHAPE;   // whole blocks along K of either product
+  if (s->flags & kNotFp4) return MOE_ERR_INVALID_ARG;
+  if (w1q == nullptr || w3q == nullptr || w2q == nullptr || s1 == nullptr || s3 == nullptr || s2 == nullptr) return MOE_ERR_INVALID_ARG;
+  if (!aligned(w1q, 128) || !aligned(w3q, 128) || !aligned(w2q, 128) || !aligned(s1, 16) || !aligned(s3, 16) || !aligned(s2, 16))
+    return MOE_ERR_MISALIGNED;
+  return MOE_OK;
+}
+Fp4Args fp4_args(void* ws, const WsPlan& p, const void* sx, const void* s1, const void* s3, const void* s2) {
+  return Fp4Args{static_cast<const uint8_t*>(sx), static_cast<const uint8_t*>(s1), static_cast<const uint8_t*>(s3),
+                 static_cast<const uint8_t*>(s2), at<uint8_t>(ws, p.sf_x), at<uint8_t>(ws, p.sf_h)};
+}
+}  // namespace
+}  // namespace tcmoe
+
+int moe_expert_ffn_fp4(const moe_shape_t* shape, const void* xq, const void* sx, const moe_layout_t* layout, const float* topk_w,
+                       const void* w1q, const void* s1, const void* w3q, const void* s3, const void* w2q, const void* s2, void* o,
+                       void* ws, size_t ws_bytes, void* stream) {
+  int rc = check_shape(shape);
+  if (rc != MOE_OK) return rc;
+  if ((rc = check_fp4(shape, w1q, s1, w3q, s3, w2q, s2)) != MOE_OK) return rc;
+  if (xq == nullptr || sx == nullptr || o == nullptr) return MOE_ERR_INVALID_ARG;
+  const bool in_combine = (shape->flags & MOE_FLAG_WEIGHT_IN_COMBINE) != 0;
+  if (!in_combine && topk_w == nullptr) return MOE_ERR_INVALID_ARG;
+  if ((rc = check_layout(layout)) != MOE_OK) return rc;
+  if (!aligned(xq, 128) || !aligned(o, 128) || !aligned(topk_w, 16)) return MOE_ERR_MISALIGNED;
+  WsPlan p;
+  if ((rc = check_ws(shape, ws, ws_bytes, &p)) != MOE_OK) return rc;
+  if (!have_device()) return MOE_ERR_CUDA;
+  FfnArgs a{};
+  a.a_src = xq;
+  a.a_rows = shape->T * (shape->k < shape->G ? shape->k : shape->G);   // capacity of the dispatched buffer
+  a.gather_idx = layout->row_src;
+  a.gather_div = 1;
+  a.w1 = w1q;
+  a.w3 = w3q;
+  a.w2 = w2q;
+  a.xs = at<void>(ws, p.o);
+  a.h = at<void>(ws, p.h);
+  a.o = o;
+  a.topk_w = in_combine ? nullptr : topk_w;
+  a.row_pair = layout->row_pair;
+  a.expert_offsets = layout->expert_offsets;
+  a.status = at<int32_t>(ws, p.status);
+  TCMOE_CUDA(launch_expert_ffn_fp4(to_shape(*shape), a, fp4_args(ws, p, sx, s1, s3, s2), static_cast<cudaStream_t>(stream)));
+  return MOE_OK;
+}
+
 int moe_combine(const moe_shape_t* shape, const void* o, const moe_layout_t* layout, const int32_t* topk_idx,
                 const float* topk_w, void* pg, void* y, void* ws, size_t ws_bytes, void* stream) {
   int rc = check_shape(shape);
@@ -807,12 +864,12 @@ int moe_combine(const moe_shape_t* shape, const void* o, const moe_layout_t* lay
   return MOE_OK;
 }
 
-// Shared body of moe_layer and moe_layer_fp8.  fp8 == nullptr: bf16 experts, w1 / w3 / w2 are
-// [E, K, N] bf16.  Otherwise they are E4M3 codes [E, N, K] with the scales in *fp8 (sx, hq, sh are
-// filled here from the workspace).
+// Shared body of moe_layer, moe_layer_fp8 and moe_layer_fp4.  Neither fp8 nor fp4: bf16 experts, w1 / w3 / w2 are
+// [E, K, N] bf16.  Otherwise they are E4M3 codes [E, N, K] or E2M1 codes [E, N, K / 2] with the scales in *fp8 / *fp4
+// (what belongs to the activations is filled here from the workspace).
 static int layer_impl(const moe_shape_t* shape, const void* x, const float* w_gate, const float* logit_bias,
                       int64_t bias_row_stride, const void* w1, const void* w3, const void* w2, const Fp8Args* fp8,
-                      void* y, float* logits, int32_t* topk_idx, float* topk_w, const moe_layout_t* layout, void* ws,
+                      const Fp4Args* fp4, void* y, float* logits, int32_t* topk_idx, float* topk_w, const moe_layout_t* layout, void* ws,
                       size_t ws_bytes, void* stream) {
   int rc = check_shape(shape);
   if (rc != MOE_OK) return rc;
@@ -823,6 +880,7 @@ static int layer_impl(const moe_shape_t* shape, const void* x, const float* w_ga
     if (fp8->s1 == nullptr || fp8->s3 == nullptr || fp8->s2 == nullptr) return MOE_ERR_INVALID_ARG;
     if (!aligned(fp8->s1, 4) || !aligned(fp8->s3, 4) || !aligned(fp8->s2, 4)) return MOE_ERR_MISALIGNED;
   }
+  if (fp4 != nullptr && (rc = check_fp4(shape, w1, fp4->s1, w3, fp4->s3, w2, fp4->s2)) != MOE_OK) return rc;
   if (x == nullptr || w_gate == nullptr || w1 == nullptr || w3 == nullptr || w2 == nullptr || y == nullptr)
     return MOE_ERR_INVALID_ARG;
   if (bias_row_stride != 0 && bias_row_stride != shape->E) return MOE_ERR_INVALID_ARG;
@@ -871,6 +929,14 @@ static int layer_impl(const moe_shape_t* shape, const void* x, const float* w_ga
     a.a_src = at<void>(ws, p.xq);
     TCMOE_CUDA(launch_quantize_rows(x, s.T, s.d, at<void>(ws, p.xq), at<float>(ws, p.sx), st));
   }
+  Fp4Args q4{};
+  if (fp4 != nullptr) {   // codes of x [T, d / 2], then their scales [T, d / 32], where the FP8 form keeps its copy of x
+    uint8_t* xq = at<uint8_t>(ws, p.xq);
+    uint8_t* sx = xq + (size_t)s.T * s.d / 2;
+    q4 = fp4_args(ws, p, sx, fp4->s1, fp4->s3, fp4->s2);
+    a.a_src = xq;
+    TCMOE_CUDA(launch_quantize_rows_fp4(x, s.T, s.d, xq, sx, st));
+  }
   a.a_rows = s.T;
   a.gather_idx = L.row_pair;   // token of expert row r = row_pair[r] / k
   a.gather_div = s.k;
@@ -910,7 +976,8 @@ static int layer_impl(const moe_shape_t* shape, const void* x, const float* w_ga
     TCMOE_CUDA(launch_expert_ffn(s, a, st));
     return MOE_OK;
   }
-  TCMOE_CUDA(fp8 != nullptr ? launch_expert_ffn_fp8(s, a, q, st) : launch_expert_ffn(s, a, st));
+  if (fp4 != nullptr) a.xs = a.o;   // the sorted codes of x: GEMM-1 has read them when GEMM-2 writes o
+  TCMOE_CUDA(fp4 != nullptr ? launch_expert_ffn_fp4(s, a, q4, st) : fp8 != nullptr ? launch_expert_ffn_fp8(s, a, q, st) : launch_expert_ffn(s, a, st));
   TCMOE_CUDA(launch_combine(s, a.o, L, idx, tw, nullptr, y, status, st, true));
   return MOE_OK;
 }
@@ -918,7 +985,7 @@ static int layer_impl(const moe_shape_t* shape, const void* x, const float* w_ga
 int moe_layer(const moe_shape_t* shape, const void* x, const float* w_gate, const float* logit_bias,
               int64_t bias_row_stride, const void* w1, const void* w3, const void* w2, void* y, float* logits,
               int32_t* topk_idx, float* topk_w, const moe_layout_t* layout, void* ws, size_t ws_bytes, void* stream) {
-  return layer_impl(shape, x, w_gate, logit_bias, bias_row_stride, w1, w3, w2, nullptr, y, logits, topk_idx, topk_w,
+  return layer_impl(shape, x, w_gate, logit_bias, bias_row_stride, w1, w3, w2, nullptr, nullptr, y, logits, topk_idx, topk_w,
                     layout, ws, ws_bytes, stream);
 }
 
@@ -930,8 +997,19 @@ int moe_layer_fp8(const moe_shape_t* shape, const void* x, const float* w_gate, 
   q.s1 = s1;
   q.s3 = s3;
   q.s2 = s2;
-  return layer_impl(shape, x, w_gate, logit_bias, bias_row_stride, w1q, w3q, w2q, &q, y, logits, topk_idx, topk_w,
+  return layer_impl(shape, x, w_gate, logit_bias, bias_row_stride, w1q, w3q, w2q, &q, nullptr, y, logits, topk_idx, topk_w,
                     layout, ws, ws_bytes, stream);
+}
+
+int moe_layer_fp4(const moe_shape_t* shape, const void* x, const float* w_gate, const float* logit_bias, int64_t bias_row_stride,
+                  const void* w1q, const void* s1, const void* w3q, const void* s3, const void* w2q, const void* s2, void* y,
+                  float* logits, int32_t* topk_idx, float* topk_w, const moe_layout_t* layout, void* ws, size_t ws_bytes, void* stream) {
+  Fp4Args q{};
+  q.s1 = static_cast<const uint8_t*>(s1);
+  q.s3 = static_cast<const uint8_t*>(s3);
+  q.s2 = static_cast<const uint8_t*>(s2);
+  return layer_impl(shape, x, w_gate, logit_bias, bias_row_stride, w1q, w3q, w2q, nullptr, &q, y, logits, topk_idx, topk_w, layout, ws,
+                    ws_bytes, stream);
 }
 
 int moe_layer_host(const moe_shape_t* shape, const void* x_host, void* x_dev, const float* w_gate,

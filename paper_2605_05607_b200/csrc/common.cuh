@@ -243,6 +243,15 @@ struct Fp8Args {
   float* sh;                  // [P] scratch: row scales of h
 };
 cudaError_t launch_expert_ffn_fp8(const Shape& s, const FfnArgs& a, const Fp8Args& q, cudaStream_t st);
+// FP4 form (ffn_fp4.cu): a.a_src / a.w1 / a.w3 / a.w2 hold E2M1 codes, two per byte (weights [E, N, K / 2]); a.xs takes the sorted rows, a.h the
+// codes of h
+struct Fp4Args {
+  const uint8_t* sx;            // [a_rows, d / 32]
+  const uint8_t *s1, *s3, *s2;  // scale chunks of the weights
+  uint8_t *sfx, *sfh;           // scratch: scale chunks of the row tiles of x and of h
+};
+long long fp4_row_tiles(const Shape& s);   // row tiles at most
+cudaError_t launch_expert_ffn_fp4(const Shape& s, const FfnArgs& a, const Fp4Args& q, cudaStream_t st);
 // ep.cu: the two steps that expert parallelism across GPUs adds to the single-GPU path
 cudaError_t launch_ep_pack(const Shape& s, const int32_t* topk_idx, const float* topk_w, const Layout& L,
                            int32_t* send_idx, float* send_w, cudaStream_t st);

@@ -1,0 +1,407 @@
+// FP4 form of the expert FFN: E2M1 elements, a power of two per 32 of K, on the block-scaled tensor-core instructions (tcgen05
+// kind::mxf4), which take the scales along and accumulate the scaled products in fp32:
+//     GEMM-1  h[r, n] = silu(a_r . W1[e][:, n]) * (a_r . W3[e][:, n]), quantised in the epilogue: h exists in 4 bits only
+//     GEMM-2  o[r, n] = w_r * (h_r . W2[e][:, n])
+//
+// The weights are the M side of the UMMAs (two of 128 columns: the same columns of W1 and of W3, or neighbouring ones of W2), the tile's rows
+// the N side, rounded up to 16: experts of a few rows, which stream weights, pay for no padded rows, and 32 neighbouring columns of h
+// lie in the 32 lanes of a warp, which quantises them without shared memory.
+//
+// A pipeline stage holds 256 of K: 128 bytes per row of either operand (packed, 128-byte swizzle, by TMA) and their scales in chunks of 128
+// rows x 4 (512 bytes, by untiled bulk copies, in the layout that tcgen05.cp spreads over TMEM).  The scales' TMEM columns belong to the
+// stage: when a stage is filled again, the UMMAs that read its scales have completed.
+//
+// TMEM: two accumulator buffers of 2 x 96 columns, then 24 columns of scales per stage.  Warp roles: 0-7 epilogue, 8 TMA, 9 UMMA and TMEM
+// owner.  One persistent CTA per SM; every wait is bounded.
+#include "ffn_common.cuh"
+#include "ffn_fp4.cuh"
+
+#include <atomic>
+
+namespace tcmoe {
+namespace ffn {
+namespace {
+
+constexpr int F4_BK = 256;                          // K per stage
+constexpr int W_BYTES = 128 * 128;                  // one half of the weight tile: 128 columns x 256 of K
+constexpr int X_BYTES = 128 * F4_ROWS;              // the tile's rows
+constexpr int SF_BYTES = 1024;                      // scales of 128 rows x 256 of K
+constexpr int STAGE_BYTES = 2 * W_BYTES + X_BYTES + 3 * SF_BYTES;   // W W X sfX sfW sfW
+constexpr int NSTAGE = 4;
+constexpr int SF_COLS = 24;                         // TMEM columns of a stage's scales
+constexpr int BUF_COLS = 2 * F4_ROWS;               // of an accumulator buffer
+constexpr int SF_TMEM = 2 * BUF_COLS;
+static_assert(SF_TMEM + NSTAGE * SF_COLS <= 512, "TMEM");
+static_assert(X_BYTES % 1024 == 0, "swizzle atoms");
+constexpr int NUM_BARS = 2 * NSTAGE + 4;
+constexpr int EPI_WARPS = 8, TMA_WARP = EPI_WARPS, MMA_WARP = EPI_WARPS + 1;
+constexpr int THREADS = (EPI_WARPS + 2) * 32;
+constexpr int TABLE_BYTES = (2 * (MAX_E + 1) * 4 + 15) & ~15;
+constexpr int SMEM_BYTES = 1024 + NSTAGE * STAGE_BYTES + NUM_BARS * 8 + 64 + TABLE_BYTES;
+static_assert(SMEM_BYTES <= 232448, "shared memory of an SM");
+constexpr uint32_t HINT = 1000;
+
+// Instruction descriptor of kind::mxf4: A, B E2M1, both K-major, scales E8M0, M = 128 (weights), N = n rows; the scale pair of an
+// instruction's 64 of K is bytes id, id + 1 of the columns.
+__host__ __device__ constexpr uint32_t idesc_f4(int n, int id) {
+  return ((uint32_t)id << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | (1u << 23) | ((uint32_t)(128 >> 7) << 27) |
+         ((uint32_t)id << 29);
+}
+// 32 rows of 16 bytes in shared memory, no swizzle: eight-row groups 128 bytes apart
+__device__ __forceinline__ uint64_t scale_desc(uint32_t smem_addr) {
+  return (uint64_t)((smem_addr & 0x3FFFF) >> 4) | ((uint64_t)(128 >> 4) << 16) | ((uint64_t)(128 >> 4) << 32) | (1ull << 46);
+}
+
+// Tiles of F4_ROWS rows per expert, exclusive prefix, by the first warp of the block (tp[E] = all of them).
+__device__ __forceinline__ void tile_table(const int32_t* expert_offsets, int E, int* tp, int* eoff, int lane) {
+  int base = 0;
+  for (int e0 = 0; e0 < E; e0 += 32) {
+    const int e = e0 + lane;
+    const int lo = __ldcg(expert_offsets + min(e, E)), hi = __ldcg(expert_offsets + min(e + 1, E));
+    const int tiles = (hi - lo + F4_ROWS - 1) / F4_ROWS;
+    int sum = tiles;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const int u = __shfl_up_sync(0xFFFFFFFFu, sum, off);
+      if (lane >= off) sum += u;
+    }
+    if (e < E) {
+      tp[e] = base + sum - tiles;
+      eoff[e] = lo;
+      if (e == E - 1) {
+        tp[E] = base + sum;
+        eoff[E] = hi;
+      }
+    }
+    base += __shfl_sync(0xFFFFFFFFu, sum, 31);
+  }
+}
+
+struct F4Tile {
+  int e, mt, row0, rows, c0, halves;   // expert, row tile over all experts, first row, rows; first 128-column chunk, halves in use
+};
+
+template <bool GLU>
+__global__ void __launch_bounds__(THREADS, 1)
+ffn_fp4_kernel(const __grid_constant__ CUtensorMap map_wa, const __grid_constant__ CUtensorMap map_wb,
+               const __grid_constant__ F4RowMaps xmaps, const F4Params p) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + NSTAGE * STAGE_BYTES);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + NUM_BARS);
+  int* abort_s = reinterpret_cast<int*>(tmem_slot + 1);
+  int* tp_s = reinterpret_cast<int*>(tmem_slot + 16);
+  int* eoff_s = tp_s + (MAX_E + 1);
+  const uint32_t smem_base = ptx::smem_u32(smem), bar_base = ptx::smem_u32(bars);
+  auto full_bar = [&](int s) { return bar_base + 8u * s; };
+  auto empty_bar = [&](int s) { return bar_base + 8u * (NSTAGE + s); };
+  auto tfull_bar = [&](int b) { return bar_base + 8u * (2 * NSTAGE + b); };
+  auto tempty_bar = [&](int b) { return bar_base + 8u * (2 * NSTAGE + 2 + b); };
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < NSTAGE; ++s) {
+      ptx::mbar_init(full_bar(s), 1);    // TMA thread (expect_tx)
+      ptx::mbar_init(empty_bar(s), 1);   // tcgen05.commit
+    }
+    for (int b = 0; b < 2; ++b) {
+      ptx::mbar_init(tfull_bar(b), 1);             // tcgen05.commit
+      ptx::mbar_init(tempty_bar(b), EPI_WARPS);    // one lane per epilogue warp
+    }
+    ptx::fence_mbar_init();
+  }
+  if (warp == TMA_WARP && lane == 0) {
+    ptx::prefetch_tensormap(&map_wa);
+    ptx::prefetch_tensormap(&map_wb);
+  }
+  if (warp == MMA_WARP) {
+    ptx::tmem_alloc(ptx::smem_u32(tmem_slot), 512);
+    ptx::tmem_relinquish();
+  }
+  grid_dependency_sync();   // nothing above touches global data
+  if (warp == 0) tile_table(p.expert_offsets, p.E, tp_s, eoff_s, lane);
+  if (threadIdx.x == 32) *abort_s = p.status[ST_ABORT];
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  const int n_tiles = GLU ? p.NC : (p.NC + 1) / 2;   // column tiles: one chunk of W1 and of W3, or two of W2
+  const int total = tp_s[p.E] * n_tiles;
+  const int KB = (p.K + F4_BK - 1) / F4_BK;
+  volatile int* abort_flag = abort_s;
+  const volatile int* global_abort = p.status + ST_ABORT;
+  auto timeout = [&](int detail) {
+    report_error(p.status, DEV_TIMEOUT, GLU ? KID_GEMM1 : KID_GEMM2, detail, blockIdx.x);
+    p.status[ST_ABORT] = 1;
+    *abort_flag = 1;
+  };
+  // expert by expert, and inside one column tile by column tile, rows fastest: CTAs that run together share weights in L2
+  auto tile_of = [&](int w) {
+    int lo = 0, hi = p.E;   // tp[lo] * n_tiles <= w < tp[hi] * n_tiles
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (tp_s[mid] * n_tiles <= w) lo = mid; else hi = mid;
+    }
+    const int local = w - tp_s[lo] * n_tiles, mts = tp_s[lo + 1] - tp_s[lo];
+    F4Tile t;
+    t.e = lo;
+    const int m = local % mts;
+    t.mt = tp_s[lo] + m;
+    t.row0 = eoff_s[lo] + m * F4_ROWS;
+    t.rows = min(F4_ROWS, eoff_s[lo + 1] - t.row0);
+    const int c = local / mts;
+    t.c0 = GLU ? c : 2 * c;
+    t.halves = GLU ? 2 : min(2, p.NC - t.c0);
+    return t;
+  };
+
+  if (warp < EPI_WARPS) {
+    // ================================ epilogue: lane = column, TMEM column = row ================================
+    const int quarter = warp & 3, turn = warp >> 2, odd = lane & 1;
+    int tl = 0;
+    for (int w = blockIdx.x; w < total && !*abort_flag; w += gridDim.x, ++tl) {
+      const F4Tile t = tile_of(w);
+      const int buf = tl & 1;
+      if (!ptx::mbar_wait_warp<true>(tfull_bar(buf), (tl >> 1) & 1, abort_flag, global_abort)) { timeout(1); break; }
+      ptx::tc_fence_after();
+      const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * BUF_COLS);
+      const int c = quarter * 32 + lane;
+#pragma unroll 1
+      for (int r0 = turn * 16; r0 < t.rows; r0 += 32) {   // the two warps of a quarter take turns
+        uint32_t a[16], b[16];
+        ptx::tmem_ld16(taddr + r0, a);
+        ptx::tmem_ld16(taddr + F4_ROWS + r0, b);
+        ptx::tmem_ld_wait_on(a, b);
+        if (GLU) {
+          // block of 32 columns = the warp, one row at a time; eight rows' codes are then exchanged so that each lane has eight columns of one
+          const bool in = t.c0 * 128 + quarter * 32 < p.N;   // N is a multiple of 32
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            uint32_t mine = 0, bytes[2] = {0u, 0u};   // this column's codes of eight rows; scale bytes of the rows
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const float h = silu_mul(__uint_as_float(a[g * 8 + i]), __uint_as_float(b[g * 8 + i]));
+              const uint32_t top = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(h) & 0x7FFFFFFFu);
+              const uint32_t sb = fp4::scale_byte(__uint_as_float(top));
+              mine |= fp4::code(h * fp4::inverse(sb)) << (4 * i);
+              bytes[i >> 2] |= sb << (8 * (i & 3));
+            }
+            mine = fp4::transpose8(mine, lane);     // lane l of eight: row l, the columns of its group of eight
+            const int row = r0 + g * 8 + (lane & 7);
+            if (row < t.rows) {
+              if (in)
+                p.hq[(size_t)(t.row0 + row) * (size_t)(p.N / 8) + t.c0 * 16 + quarter * 4 + (lane >> 3)] = mine;
+              if (lane < 8) {
+                uint8_t* sf = p.sfh + ((size_t)t.mt * (size_t)fp4::chunks(p.N) + t.c0) * 512 + (row & 31) * 16 + (row >> 5) * 4 + quarter;
+                sf[0] = in ? (uint8_t)(bytes[lane >> 2] >> (8 * (lane & 3))) : 127;
+                if (t.c0 + 1 == p.NC && (p.NC & 1)) sf[512] = 127;   // the chunk past the last column is part of a stage
+              }
+            }
+          }
+        } else {
+          const int mine = r0 + (lane & 15);
+          float rs = 1.f;   // gate weight of this lane's row of the 16
+          if (mine < t.rows && p.topk_w != nullptr) rs = __ldg(p.topk_w + __ldg(p.row_pair + t.row0 + mine));
+          // two rows at a time: neighbouring lanes swap, and each stores two columns of one of the rows
+          auto put = [&](float v0, float v1, int r, int col) {
+            const float got = __shfl_xor_sync(0xFFFFFFFFu, odd ? v0 : v1, 1);
+            const int row = r0 + r + odd, at = col - odd;
+            if (row < t.rows && at < p.N)
+              *reinterpret_cast<uint32_t*>(p.out + (size_t)(t.row0 + row) * (size_t)p.N + at) = odd ? pack2(got, v1) : pack2(v0, got);
+          };
+#pragma unroll
+          for (int r = 0; r < 16; r += 2) {
+            const float w0 = __shfl_sync(0xFFFFFFFFu, rs, r), w1 = __shfl_sync(0xFFFFFFFFu, rs, r + 1);
+            put(w0 * __uint_as_float(a[r]), w1 * __uint_as_float(a[r + 1]), r, t.c0 * 128 + c);
+            if (t.halves > 1) put(w0 * __uint_as_float(b[r]), w1 * __uint_as_float(b[r + 1]), r, t.c0 * 128 + 128 + c);
+          }
+        }
+      }
+      ptx::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(tempty_bar(buf));
+    }
+  } else if (warp == TMA_WARP) {
+    // ================================ TMA producer ================================
+    if (lane == 0) {
+      uint32_t it = 0;
+      for (int w = blockIdx.x; w < total && !*abort_flag; w += gridDim.x) {
+        const F4Tile t = tile_of(w);
+        const int box = (t.rows + 31) / 32;   // rows by 32; what the stage held behind them reaches no stored row
+        const uint32_t bytes = (uint32_t)(t.halves * (W_BYTES + SF_BYTES) + box * 32 * 128 + SF_BYTES);
+        const size_t wc0 = (size_t)t.e * p.NC + t.c0, wc1 = GLU ? wc0 : wc0 + 1;
+        bool ok = true;
+        for (int kb = 0; kb < KB; ++kb, ++it) {
+          const int s = it % NSTAGE;
+          if (!ptx::mbar_wait<false, HINT>(empty_bar(s), ((it / NSTAGE) & 1) ^ 1, abort_flag, global_abort)) {
+            timeout(2); ok = false; break;
+          }
+          const uint32_t sw = smem_base + s * STAGE_BYTES, sx = sw + 2 * W_BYTES, sf = sx + X_BYTES, bar = full_bar(s);
+          ptx::mbar_arrive_expect_tx(bar, bytes);
+          ptx::tma_load_3d(sw, &map_wa, bar, kb * 128, t.c0 * 128, t.e);
+          ptx::bulk_load(sf + SF_BYTES, p.sfa + (wc0 * KB + kb) * SF_BYTES, SF_BYTES, bar);
+          if (t.halves > 1) {
+            ptx::tma_load_3d(sw + W_BYTES, &map_wb, bar, kb * 128, GLU ? t.c0 * 128 : t.c0 * 128 + 128, t.e);
+            ptx::bulk_load(sf + 2 * SF_BYTES, p.sfb + (wc1 * KB + kb) * SF_BYTES, SF_BYTES, bar);
+          }
+          ptx::tma_load_2d(sx, &xmaps.m[box - 1], bar, kb * 128, t.row0);
+          ptx::bulk_load(sf, p.sfx + ((size_t)t.mt * KB + kb) * SF_BYTES, SF_BYTES, bar);
+        }
+        if (!ok) break;
+      }
+    }
+  } else if (warp == MMA_WARP) {
+    // ================================ UMMA issuer: the warp walks the loop, one elected lane issues ================================
+    const bool elected = ptx::elect_one();
+    const uint32_t base = __shfl_sync(0xFFFFFFFFu, smem_base, 0), tmem = __shfl_sync(0xFFFFFFFFu, tmem_base, 0);
+    const uint64_t w_desc = desc_at(desc_base(16, 1024), base), x_desc = desc_at(desc_base(16, 1024), base + 2 * W_BYTES);
+    const uint64_t sf_desc = scale_desc(base + 2 * W_BYTES + X_BYTES);
+    int s = 0, tl = 0;
+    uint32_t ph = 0;
+    bool ok = true;
+    for (int w = blockIdx.x; ok && w < total && !*abort_flag; w += gridDim.x, ++tl) {
+      const int buf = tl & 1;
+      const F4Tile t = tile_of(w);
+      if (!ptx::mbar_wait(tempty_bar(buf), ((tl >> 1) & 1) ^ 1, abort_flag, global_abort)) { timeout(3); break; }
+      ptx::tc_fence_after();
+      const uint32_t d = tmem + (uint32_t)(buf * BUF_COLS);
+      const int n = (t.rows + 15) & ~15;
+      const uint32_t id0 = idesc_f4(n, 0), id1 = idesc_f4(n, 2);
+      for (int kb = 0; kb < KB; ++kb) {
+        if (!ptx::mbar_wait(full_bar(s), ph, abort_flag, global_abort)) { timeout(4); ok = false; break; }
+        ptx::tc_fence_after();
+        if (elected) {
+          const uint64_t so = (uint64_t)(s * (STAGE_BYTES >> 4));
+          const uint32_t sf = tmem + (uint32_t)(SF_TMEM + s * SF_COLS);   // X chunks, W half 0 chunks, W half 1 chunks: four columns each
+#pragma unroll
+          for (int i = 0; i < 6; ++i)
+            if (i < 4 || t.halves > 1) ptx::tmem_copy_scales(sf + 4 * i, sf_desc + so + (uint64_t)(i * (512 >> 4)));
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {   // 64 of K: 32 bytes inside the swizzle row
+            const uint32_t id = (k & 1) ? id1 : id0, ch = (uint32_t)(4 * (k >> 1));
+            ptx::umma_f4(d, w_desc + so + 2 * k, x_desc + so + 2 * k, id, sf + 8 + ch, sf + ch, (kb | k) != 0);
+            if (t.halves > 1)
+              ptx::umma_f4(d + F4_ROWS, w_desc + so + (W_BYTES >> 4) + 2 * k, x_desc + so + 2 * k, id, sf + 16 + ch, sf + ch, (kb | k) != 0);
+          }
+          ptx::umma_commit(empty_bar(s));   // free the stage when these UMMAs have read it
+        }
+        if (++s == NSTAGE) { s = 0; ph ^= 1u; }
+      }
+      if (ok && elected) ptx::umma_commit(tfull_bar(buf));
+    }
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  if (*abort_flag || *global_abort) {
+    // abort path only: give bulk copies and UMMAs still in flight time to land before the CTA retires
+    for (int i = 0; i < 64; ++i) __nanosleep(1000);
+  }
+  __syncthreads();
+  if (warp == MMA_WARP) {
+    ptx::tc_fence_after();
+    ptx::tmem_dealloc(tmem_base, 512);
+  }
+}
+
+// Quantised rows, gathered into expert-sorted order, and their scales into the chunks of the row tiles.  A warp per row; which expert a row
+// belongs to, and which tile of all, comes from one pass over the offsets.
+__global__ void __launch_bounds__(256) fp4_sort_kernel(const uint4* __restrict__ xq, const uint8_t* __restrict__ sx, int a_rows,
+                                                       const int32_t* __restrict__ gather_idx, int gather_div,
+                                                       const int32_t* __restrict__ expert_offsets, int E, int K, int capacity, uint4* xs,
+                                                       uint8_t* sfx, int32_t* status) {
+  grid_dependency_sync();
+  const int lane = threadIdx.x & 31;
+  const int KB = K / 32, words = fp4::chunks(K);   // scale bytes of a row, and its 4-byte words in the chunks
+  const int rows = min(__ldg(expert_offsets + E), capacity);
+  for (int r = blockIdx.x * 8 + (threadIdx.x >> 5); r < rows; r += gridDim.x * 8) {
+    int src = __ldg(gather_idx + r);
+    if (gather_div > 1) src /= gather_div;
+    int before = 0, first = 0;   // tiles of the experts that end at or before this row; first row of its own
+    for (int e = lane; e < E; e += 32) {
+      const int lo = __ldg(expert_offsets + e), hi = __ldg(expert_offsets + e + 1);
+      if (hi <= r) before += (hi - lo + F4_ROWS - 1) / F4_ROWS;
+      else if (lo <= r) first = lo;
+    }
+    before = __reduce_add_sync(0xFFFFFFFFu, before);
+    first = __reduce_max_sync(0xFFFFFFFFu, first);
+    if (src < 0 || src >= a_rows) {
+      if (lane == 0) report_error(status, DEV_INDEX_OUT_OF_RANGE, KID_GEMM1, src, r);
+      continue;
+    }
+    const uint4* from = xq + (size_t)src * KB;
+    uint4* to = xs + (size_t)r * KB;
+    for (int v = lane; v < KB; v += 32) to[v] = __ldg(from + v);
+    const int mt = before + (r - first) / F4_ROWS, lr = (r - first) % F4_ROWS;
+    uint8_t* sf = sfx + (size_t)mt * words * 512 + (lr & 31) * 16 + (lr >> 5) * 4;
+    const uint8_t* s = sx + (size_t)src * KB;
+    for (int c = lane; c < words; c += 32) {
+      uint32_t v = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v |= (4 * c + i < KB ? (uint32_t)__ldg(s + 4 * c + i) : 127u) << (8 * i);
+      *reinterpret_cast<uint32_t*>(sf + (size_t)c * 512) = v;
+    }
+  }
+}
+
+template <bool GLU>
+cudaError_t launch_gemm(const F4Params& p, const void* wa, const void* wb, const void* rows, long long n_rows, cudaStream_t st) {
+  static std::atomic<bool> attr_set[MAX_DEVICES];   // per device; setting it twice is harmless
+  const int dev = current_device();
+  if (!attr_set[dev].load(std::memory_order_acquire)) {
+    const cudaError_t e = cudaFuncSetAttribute(ffn_fp4_kernel<GLU>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
+    if (e != cudaSuccess) return e;
+    attr_set[dev].store(true, std::memory_order_release);
+  }
+  CUtensorMap m_a, m_b;
+  F4RowMaps x;
+  if (!make_weight_map_fp8(&m_a, wa, p.E, p.N, p.K / 2, 128) || !make_weight_map_fp8(&m_b, wb, p.E, p.N, p.K / 2, 128)) return cudaErrorInvalidValue;
+  for (int i = 0; i < F4_ROWS / 32; ++i)
+    if (!make_act_map(&x.m[i], rows, n_rows, p.K / 2, true, 32 * (i + 1))) return cudaErrorInvalidValue;
+  ProfileScope prof(GLU ? KID_GEMM1 : KID_GEMM2, st);
+  return launch_pdl(ffn_fp4_kernel<GLU>, dim3(sm_count()), dim3(THREADS), SMEM_BYTES, st, m_a, m_b, x, p);
+}
+
+}  // namespace
+}  // namespace ffn
+
+long long fp4_row_tiles(const Shape& s) {
+  const long long P = (long long)s.T * s.k;
+  return P / ffn::F4_ROWS + (s.E < P ? s.E : P);
+}
+
+cudaError_t launch_expert_ffn_fp4(const Shape& s, const FfnArgs& a, const Fp4Args& q, cudaStream_t st) {
+  if (s.T == 0) return cudaSuccess;
+  const int P = s.T * s.k;
+  const int blocks = (P + 7) / 8, cap = sm_count() * 8;
+  cudaError_t e = launch_pdl(ffn::fp4_sort_kernel, dim3(blocks < cap ? blocks : cap), dim3(256), 0, st, static_cast<const uint4*>(a.a_src),
+                             q.sx, a.a_rows, a.gather_idx, a.gather_div, a.expert_offsets, s.E, s.d, P, static_cast<uint4*>(a.xs), q.sfx, a.status);
+  if (e != cudaSuccess) return e;
+  ffn::F4Params g1{};
+  g1.expert_offsets = a.expert_offsets;
+  g1.E = s.E;
+  g1.K = s.d;
+  g1.N = s.f;
+  g1.NC = (s.f + 127) / 128;
+  g1.sfx = q.sfx;
+  g1.sfa = q.s1;
+  g1.sfb = q.s3;
+  g1.hq = static_cast<uint32_t*>(a.h);
+  g1.sfh = q.sfh;
+  g1.status = a.status;
+  if ((e = ffn::launch_gemm<true>(g1, a.w1, a.w3, a.xs, P, st)) != cudaSuccess) return e;
+  ffn::F4Params g2{};
+  g2.expert_offsets = a.expert_offsets;
+  g2.E = s.E;
+  g2.K = s.f;
+  g2.N = s.d;
+  g2.NC = (s.d + 127) / 128;
+  g2.sfx = q.sfh;
+  g2.sfa = g2.sfb = q.s2;
+  g2.out = static_cast<__nv_bfloat16*>(a.o);
+  g2.topk_w = a.topk_w;
+  g2.row_pair = a.row_pair;
+  g2.status = a.status;
+  return ffn::launch_gemm<false>(g2, a.w2, a.w2, a.h, P, st);
+}
+
+}  // namespace tcmoe

@@ -99,6 +99,12 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* map, uint3
       "[%2];" ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2)
       : "memory");
 }
+// untiled: `bytes` (a multiple of 16) from a 16-byte aligned address
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes),
+               "r"(bar)
+               : "memory");
+}
 // ---- TMA tiled stores: read from shared memory by the async proxy (fence_proxy_async_smem after the writes), tracked by the
 // bulk groups of the issuing thread ------------------------------------------------------------------------------
 __device__ __forceinline__ void tma_store_3d(const void* map, uint32_t src, int c0, int c1, int c2) {
@@ -166,6 +172,22 @@ __device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint64_t a_desc, uint64
       "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
       ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
       : "memory");
+}
+// The same for packed 4-bit operands (E2M1) with a power-of-two scale per 32 of K on both sides (the scales in TMEM), K = 64 per
+// instruction.  Which two of a column's four scale bytes it takes is in the instruction descriptor.
+__device__ __forceinline__ void umma_f4(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t sfa_tmem,
+                                        uint32_t sfb_tmem, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %6, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sfa_tmem), "r"(sfb_tmem), "r"(accumulate)
+      : "memory");
+}
+// 512 bytes of shared memory (32 rows of 16) -> four TMEM columns, the same 32 lanes in every quarter: how scales reach TMEM.  UMMAs issued
+// after it by the same thread see them.
+__device__ __forceinline__ void tmem_copy_scales(uint32_t taddr, uint64_t desc) {
+  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
 }
 // the mbarrier receives one arrival when every UMMA issued so far by this thread has finished
 __device__ __forceinline__ void umma_commit(uint32_t bar) {

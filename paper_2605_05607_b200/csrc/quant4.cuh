@@ -54,6 +54,20 @@ __device__ __forceinline__ uint32_t codes8(const float (&f)[8], float inv) {
     c |= (uint32_t)__nv_cvt_float2_to_fp4x2(make_float2(f[2 * q] * inv, f[2 * q + 1] * inv), __NV_E2M1, cudaRoundNearest) << (8 * q);
   return c;
 }
+// the code of one (scaled) value
+__device__ __forceinline__ uint32_t code(float v) {
+  return (uint32_t)__nv_cvt_float2_to_fp4x2(make_float2(v, 0.f), __NV_E2M1, cudaRoundNearest) & 15u;
+}
+// An 8 x 8 transpose of 4-bit pieces over eight neighbouring lanes: piece i of lane l becomes piece l of lane i.
+__device__ __forceinline__ uint32_t transpose8(uint32_t v, int lane) {
+  // exchange halves with the lane 4 away, then bytes with the one 2 away, then pieces with the neighbour
+  uint32_t o = __shfl_xor_sync(0xFFFFFFFFu, v, 4);
+  v = (lane & 4) ? (v & 0xFFFF0000u) | (o >> 16) : (v & 0x0000FFFFu) | (o << 16);
+  o = __shfl_xor_sync(0xFFFFFFFFu, v, 2);
+  v = (lane & 2) ? (v & 0xFF00FF00u) | ((o >> 8) & 0x00FF00FFu) : (v & 0x00FF00FFu) | ((o << 8) & 0xFF00FF00u);
+  o = __shfl_xor_sync(0xFFFFFFFFu, v, 1);
+  return (lane & 1) ? (v & 0xF0F0F0F0u) | ((o >> 4) & 0x0F0F0F0Fu) : (v & 0x0F0F0F0Fu) | ((o << 4) & 0xF0F0F0F0u);
+}
 __device__ __forceinline__ void values8(uint32_t codes, float scale, float (&f)[8]) {
 #pragma unroll
   for (int q = 0; q < 4; ++q) {

@@ -113,3 +113,210 @@ def test_quantize_weights_bit_exact(E, K, N):
     B.moe_dequantize_weights_fp4(q, s, back)
     want = np.stack([Q.dequantize_rows(q_ref[e], s_ref[e]).T for e in range(E)])
     assert np.array_equal(f64(back), want)
+
+
+def routed(rows_per_expert, k=1, d=128, f=128, seed=0, G=1, flags=0):
+    """A batch of T tokens whose experts hold the given rows (k = 1), or T random tokens over E experts; its layout by moe_dispatch."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    if k == 1:
+        E, T = len(rows_per_expert), sum(rows_per_expert)
+        idx = torch.repeat_interleave(torch.arange(E, device="cuda"), torch.tensor(rows_per_expert, device="cuda")).int().view(T, 1)
+        idx = idx[torch.randperm(T, generator=g, device="cuda")]
+    else:
+        T, E = rows_per_expert
+        score = torch.rand(T, E, generator=g, device="cuda") - 0.5 * torch.arange(E, device="cuda") / E
+        idx = score.topk(k, dim=1).indices.int()
+        if flags & B.MOE_FLAG_SPARSE_TOPK:
+            idx[torch.rand(T, k, generator=g, device="cuda") < 0.3] = -1
+    shape = B.MoEShape(T, d, f, E, k, G, 0, flags)
+    ws, lay = B.alloc_workspace(shape), B.alloc_layout(shape)
+    x = torch.randn(T, d, generator=g, device="cuda").bfloat16()
+    xg = torch.zeros(T * min(k, G), d, device="cuda").bfloat16()
+    B.moe_dispatch(shape, x, idx.contiguous(), lay, xg, ws)
+    w = torch.rand(T, k, generator=g, device="cuda") + 0.1
+    wt = [torch.randn(E, K, N, generator=g, device="cuda").div(K ** 0.5).bfloat16() for K, N in ((d, f), (d, f), (f, d))]
+    return shape, ws, lay, x, xg, idx, w, wt
+
+
+def check_ffn(shape, ws, lay, xg, w, wt, weighted=True):
+    P, E = shape.T * shape.k, shape.E
+    xq, sx = rows_fp4(xg)
+    q = [weights_fp4(v) for v in wt]
+    o = torch.full((P + 3, shape.d), 7.0, device="cuda").bfloat16()
+    B.moe_expert_ffn_fp4(shape, xq, sx, lay, w if weighted else None, *[t for pair in q for t in pair], o, ws)
+    assert B.moe_status(ws)[0] == 0
+    off = lay.expert_offsets[: E + 1].cpu().numpy()
+    n = int(off[E])
+    hl = {"expert_offsets": off, "row_pair": lay.row_pair.cpu().numpy()[:n], "row_src": lay.row_src.cpu().numpy()[:n]}
+    ref_w = [Q.quantize_weights(f64(v)) for v in wt]
+    ref, tol = Q.expert_ffn_fp4(*Q.quantize_rows(f64(xg)), hl, w.cpu().numpy() if weighted else None, *[t for pair in ref_w for t in pair])
+    got = f64(o)
+    assert (np.abs(got[:n] - ref) <= tol + 2.0 ** -8 * (np.abs(ref) + tol)).all(), np.abs(got[:n] - ref).max()
+    assert (got[n:] == 7.0).all()                   # rows behind the last one are left as they were
+    # and not only within the allowance: nearly every row differs by the rounding of o alone
+    err = np.linalg.norm(got[:n] - ref) / max(np.linalg.norm(ref), 1e-300)
+    assert err <= 5e-3, err
+    return o
+
+
+SMALL = [(1,), (1, 0, 3), (16, 17), (33, 1, 95, 96), (97, 192, 193), (0, 0, 5), (300,), (31, 32, 64, 65, 128, 129)]
+
+
+@pytest.mark.parametrize("counts", SMALL, ids=str)
+@pytest.mark.parametrize("d,f", [(32, 32), (256, 128), (288, 160), (512, 384), (96, 1056), (1056, 96)])
+def test_expert_ffn_fp4_by_rows_per_expert(counts, d, f):
+    shape, ws, lay, x, xg, idx, w, wt = routed(counts, d=d, f=f, seed=sum(counts) + d + f)
+    check_ffn(shape, ws, lay, xg, w, wt)
+
+
+@pytest.mark.parametrize("T,E,k,G,d,f", [(5, 4, 2, 2, 64, 96), (200, 16, 4, 4, 320, 416), (700, 8, 3, 8, 512, 256), (64, 128, 8, 8, 128, 64),
+                                         (1500, 6, 2, 3, 288, 544)])
+@pytest.mark.parametrize("flags", [0, B.MOE_FLAG_WEIGHT_IN_COMBINE, B.MOE_FLAG_SPARSE_TOPK], ids=["plain", "weight-in-combine", "sparse"])
+def test_expert_ffn_fp4_routed(T, E, k, G, d, f, flags):
+    shape, ws, lay, x, xg, idx, w, wt = routed((T, E), k, d, f, T, G, flags)
+    check_ffn(shape, ws, lay, xg, w, wt, weighted=not flags & B.MOE_FLAG_WEIGHT_IN_COMBINE)
+
+
+def quantised(wt):
+    return [t for v in wt for t in weights_fp4(v)]
+
+
+@pytest.mark.parametrize("T,E,k,G,d,f,score", [(1, 4, 2, 2, 64, 32, 0), (50, 16, 4, 4, 320, 416, 1), (900, 8, 2, 8, 512, 256, 0), (333, 128, 8, 8, 96, 160, 1)])
+@pytest.mark.parametrize("flags", [0, B.MOE_FLAG_WEIGHT_IN_COMBINE], ids=["plain", "weight-in-combine"])
+def test_layer_fp4_matches_its_oracle(T, E, k, G, d, f, score, flags):
+    cfg = H.synth.MoEConfig("fp4", T=T, d=d, f=f, E=E, k=k, G=G, score_fn=score, seed=T + E)
+    run = H.Run(cfg, flags)
+    t = run.t
+    wt = [t["w1"], t["w3"], t["w2"]]
+    lay_dev = B.alloc_layout(run.shape)
+    for _ in range(2):
+        run.y.fill_(3.0)
+        B.moe_layer_fp4(run.shape, t["x"], t["w_gate"], t["bias"], *quantised(wt), run.y, run.ws, logits=run.logits, topk_idx=run.idx,
+                        topk_w=run.w, layout=lay_dev)
+    assert run.status()[0] == 0
+    run.lay = lay_dev
+    idx_ref, _ = H.check_route(run)          # routing runs on the bf16 activations, as in moe_layer
+    lay = H.check_layout(run, idx_ref)
+    # quantising commutes with the dispatch copy: quantise x, then take the dispatched rows
+    xq, sx = Q.quantize_rows(f64(t["x"]))
+    dt = lay["disp_token"].astype(np.int64)
+    ref_w = [v for w in wt for v in Q.quantize_weights(f64(w))]
+    in_combine = bool(flags & B.MOE_FLAG_WEIGHT_IN_COMBINE)
+    o_ref, _ = Q.expert_ffn_fp4(xq[dt], sx[dt], lay, None if in_combine else run.host_w(), *ref_w)
+    _, _, y_ref = O.combine(o_ref, lay, idx_ref, run.host_w() if in_combine else None, E, G)
+    H.assert_close_out(f64(run.y)[:T], y_ref, "fp4 layer y")
+
+
+def test_layer_fp4_is_its_stages():
+    """moe_layer_fp4 against moe_route, moe_dispatch, moe_quantize_rows_fp4, moe_expert_ffn_fp4 and moe_combine: the same bits."""
+    cfg = H.synth.MoEConfig("fp4-stages", T=257, d=288, f=352, E=12, k=3, G=4, seed=8)
+    run = H.Run(cfg)
+    t, q = run.t, quantised([run.t["w1"], run.t["w3"], run.t["w2"]])
+    y = torch.zeros_like(run.y)
+    B.moe_layer_fp4(run.shape, t["x"], t["w_gate"], t["bias"], *q, y, run.ws)
+    run.route()
+    run.dispatch()
+    B.moe_expert_ffn_fp4(run.shape, *rows_fp4(run.xg), run.lay, run.w, *q, run.o, run.ws)
+    run.combine()
+    assert torch.equal(run.y, y)
+
+
+def test_norm_then_fp4_layer_then_norm():
+    """A transformer block's MoE half, as it is used: norm with the residual, the layer on its output, the next block's norm."""
+    cfg = H.synth.MoEConfig("fp4-block", T=130, d=256, f=288, E=8, k=2, G=2, seed=5)
+    run = H.Run(cfg)
+    t, q = run.t, quantised([run.t["w1"], run.t["w3"], run.t["w2"]])
+    g = torch.Generator(device="cuda").manual_seed(3)
+    rnd = lambda *s: torch.randn(*s, generator=g, device="cuda")   # noqa: E731
+    stream, attn = rnd(130, 256).bfloat16(), rnd(130, 256).bfloat16()
+    w = 1 + 0.1 * rnd(256)
+    y, out = torch.zeros_like(attn), torch.zeros_like(attn)
+    s0, a0 = f64(stream), f64(attn)
+    B.moe_rmsnorm(attn, w, 1e-6, y=y, residual=stream, res_out=stream)
+    B.moe_layer_fp4(run.shape, y, t["w_gate"], t["bias"], *q, run.y, run.ws, logits=run.logits, topk_idx=run.idx, topk_w=run.w)
+    final = torch.zeros_like(y)
+    B.moe_rmsnorm(run.y, w, 1e-6, y=final, residual=stream, res_out=out)
+    from oracle import norm_oracle as N
+    s, _, y_ref = N.rmsnorm(s0, a0, f64w := w.double().cpu().numpy(), 1e-6)
+    assert np.abs(f64(y) - y_ref).max() <= 2.0 ** -8 * np.abs(y_ref).max() + 1e-5
+    idx = run.host_idx()
+    lay = O.layout(idx, 8, 2)
+    xq, sx = Q.quantize_rows(f64(y))
+    dt = lay["disp_token"].astype(np.int64)
+    o_ref, _ = Q.expert_ffn_fp4(xq[dt], sx[dt], lay, run.host_w(), *[v for n in ("w1", "w3", "w2") for v in Q.quantize_weights(f64(t[n]))])
+    _, _, m_ref = O.combine(o_ref, lay, idx, None, 8, 2)
+    H.assert_close_out(f64(run.y)[:130], m_ref, "layer")
+    s2, _, f_ref = N.rmsnorm(m_ref, f64(stream), f64w, 1e-6)
+    H.assert_close_out(f64(out), s2, "stream")
+    H.assert_close_out(f64(final), f_ref, "next norm")
+
+
+def test_norm_feeds_fp8_experts():
+    """yq / scale of the norm are the operand of moe_expert_ffn_fp8 (one group: dispatched row = token)."""
+    from oracle import fp8_oracle as F
+    cfg = H.synth.MoEConfig("fp8-norm", T=200, d=256, f=384, E=8, k=2, G=1, seed=6)
+    run = H.Run(cfg)
+    t = run.t
+    w = (1 + 0.1 * torch.randn(256, device="cuda")).bfloat16()
+    y, yq, sc = torch.zeros_like(t["x"]), torch.zeros(200, 256, dtype=torch.uint8, device="cuda"), torch.zeros(200, device="cuda")
+    B.moe_rmsnorm(t["x"], w, 1e-6, y=y, yq=yq, scale=sc)
+    B.moe_route(run.shape, y, t["w_gate"], t["bias"], run.logits, run.idx, run.w, run.ws)
+    B.moe_dispatch(run.shape, None, run.idx, run.lay, None, run.ws)
+    wq = []
+    for name in ("w1", "w3", "w2"):
+        E, K, N = t[name].shape
+        wq += [torch.zeros(E, N, K, dtype=torch.uint8, device="cuda"), torch.zeros(E, N, device="cuda")]
+        B.moe_quantize_weights(t[name], *wq[-2:])
+    B.moe_expert_ffn_fp8(run.shape, yq, sc, run.lay, run.w, *wq, run.o, run.ws)
+    assert run.status()[0] == 0
+    lay = O.layout(run.host_idx(), 8, 1)
+    ref = F.expert_ffn_fp8(yq.cpu().numpy(), sc.cpu().numpy(), lay, run.host_w(), *[v.cpu().numpy() for v in wq])
+    H.assert_close_out(f64(run.o)[: cfg.P], ref, "fp8 experts on the norm's codes")
+
+
+def test_expert_ffn_fp4_captured_on_two_streams_and_with_an_empty_batch():
+    shape, ws, lay, x, xg, idx, w, wt = routed((150, 8), 2, 256, 288, 3)
+    q, (xq, sx) = quantised(wt), rows_fp4(xg)
+    want = torch.zeros(300, 256, device="cuda").bfloat16()
+    B.moe_expert_ffn_fp4(shape, xq, sx, lay, w, *q, want, ws)
+    side = [torch.cuda.Stream() for _ in range(2)]
+    outs, graphs = [torch.zeros_like(want) for _ in side], []
+    wss = [ws, B.alloc_workspace(shape)]                     # calls that may overlap have a workspace each
+    for s, o, v in zip(side, outs, wss):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            B.moe_expert_ffn_fp4(shape, xq, sx, lay, w, *q, o, v)
+        graphs.append(graph)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for s, graph in zip(side, graphs):
+            with torch.cuda.stream(s):
+                graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for o in outs)
+    empty = B.MoEShape(0, 256, 288, 8, 2, 1, 0, 0)
+    B.moe_expert_ffn_fp4(empty, xq, sx, lay, w, *q, want, ws)
+    assert torch.equal(outs[0], want)
+
+
+def test_fp4_a_nan_block_reaches_its_own_rows_and_columns_only():
+    shape, ws, lay, x, xg, idx, w, wt = routed((40, 30), d=128, f=96, seed=2)
+    xg[int(lay.row_src[3]), 5] = float("inf")               # a row of the first expert
+    wt[2][1, 7, 11] = float("nan")                            # column 11 of the second expert's W2
+    q, (xq, sx) = quantised(wt), rows_fp4(xg)
+    o = torch.zeros(70, 128, device="cuda").bfloat16()
+    B.moe_expert_ffn_fp4(shape, xq, sx, lay, w, *q, o, ws)
+    bad = torch.isnan(o)
+    want = torch.zeros_like(bad)
+    want[3] = True
+    want[40:, 11] = True
+    assert torch.equal(bad, want)
+
+
+def test_expert_ffn_fp4_reports_a_source_row_out_of_range():
+    shape, ws, lay, x, xg, idx, w, wt = routed((10, 20), d=64, f=64, seed=1)
+    lay.row_src[4] = 30
+    o = torch.zeros(30, 64, device="cuda").bfloat16()
+    B.moe_expert_ffn_fp4(shape, *rows_fp4(xg), lay, w, *quantised(wt), o, ws)
+    st = B.moe_status(ws)
+    assert st[0] == B.MOE_DEV_INDEX_OUT_OF_RANGE and st[2] == 30 and st[3] == 4

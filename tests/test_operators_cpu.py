@@ -1,0 +1,187 @@
+"""Refusals of the norm and the 4-bit operators, which come before any device is touched, and pins of their oracles."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import fp4_oracle as Q
+from oracle import norm_oracle as N
+from paper_2605_05607_b200 import binding as B
+from paper_2605_05607_b200 import build
+
+OK, ARG, SHAPE, SMALL, ALIGN, CUDA = (B.MOE_OK, B.MOE_ERR_INVALID_ARG, B.MOE_ERR_UNSUPPORTED_SHAPE, B.MOE_ERR_WORKSPACE_TOO_SMALL,
+                                      B.MOE_ERR_MISALIGNED, B.MOE_ERR_CUDA)
+P = 1 << 20                      # an address that is never read: every call here is refused, or finds no device
+NO_GPU = not torch.cuda.is_available()
+
+
+@pytest.fixture(scope="module")
+def L():
+    build.build_library()
+    return B.lib()
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(rows=-1), ARG), (dict(cols=0), ARG), (dict(weight=None), ARG), (dict(x=None), ARG), (dict(y=None, yq=None, scale=None), ARG),
+    (dict(yq=None), ARG), (dict(scale=None), ARG), (dict(residual=None), ARG), (dict(res_out=P), ARG), (dict(eps=-1.0), ARG),
+    (dict(eps=float("nan")), ARG), (dict(eps=float("inf")), ARG), (dict(cols=100), SHAPE), (dict(cols=16392), SHAPE), (dict(rows=1 << 40), SHAPE),
+    (dict(x=P + 2), ALIGN), (dict(weight=P + 4), ALIGN), (dict(residual=P + 8), ALIGN), (dict(y=P + 8), ALIGN), (dict(yq=P + 4), ALIGN),
+    (dict(scale=P + 2), ALIGN), (dict(rstd=P + 1), ALIGN), (dict(res_out=P + 8), ALIGN),
+], ids=str)
+def test_rmsnorm_refuses(L, change, code):
+    a = dict(x=P, residual=P, weight=P, w32=0, eps=1e-6, rows=4, cols=64, res_out=2 * P, y=P, yq=P, scale=P, rstd=P) | change
+    assert L.moe_rmsnorm(*a.values(), None) == code
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(dy=None), ARG), (dict(s=None), ARG), (dict(weight=None), ARG), (dict(rstd=None), ARG), (dict(dx=None), ARG), (dict(dw=None), ARG),
+    (dict(ws=None), ARG), (dict(rows=-1), ARG), (dict(cols=12), SHAPE), (dict(cols=16392), SHAPE), (dict(rows=1 << 31), SHAPE),
+    (dict(ws_bytes=1023), SMALL), (dict(dy=P + 8), ALIGN), (dict(dres=P + 8), ALIGN), (dict(dw=P + 4), ALIGN), (dict(ws=P + 8), ALIGN),
+    (dict(rstd=P + 2), ALIGN),
+], ids=str)
+def test_rmsnorm_backward_refuses(L, change, code):
+    a = dict(dy=P, dres=None, s=P, weight=P, w32=1, rstd=P, rows=4, cols=64, dx=P, dw=P, ws=P, ws_bytes=1024) | change
+    assert L.moe_rmsnorm_backward(*a.values(), None) == code
+
+
+def test_rmsnorm_backward_workspace(L):
+    assert B.moe_rmsnorm_backward_workspace_bytes(0, 64) == 0
+    assert B.moe_rmsnorm_backward_workspace_bytes(4, 64) == 1024
+    most = B.moe_rmsnorm_backward_workspace_bytes(1 << 20, 4096)
+    assert most == B.moe_rmsnorm_backward_workspace_bytes(1 << 30, 4096) <= 16 << 20
+    out = ctypes.c_size_t(0)
+    assert L.moe_rmsnorm_backward_workspace_bytes(4, 60, ctypes.byref(out)) == SHAPE
+    assert L.moe_rmsnorm_backward_workspace_bytes(4, 64, None) == ARG
+
+
+@pytest.mark.parametrize("fn,change,code", [
+    (fn, c, code) for fn in ("moe_quantize_rows_fp4", "moe_dequantize_rows_fp4") for c, code in (
+        (dict(src=None), ARG), (dict(rows=-1), ARG), (dict(cols=0), ARG), (dict(dst=None), ARG), (dict(cols=48), SHAPE), (dict(rows=1 << 32), SHAPE),
+        (dict(src=P + 2), ALIGN), (dict(dst=P + 2), ALIGN))
+] + [("moe_quantize_rows_fp4", dict(scale=None), ARG)], ids=str)
+def test_rows_fp4_refuse(L, fn, change, code):
+    a = dict(src=P, rows=4, cols=64, dst=P, scale=P) | change
+    order = ("src", "rows", "cols", "dst", "scale") if fn == "moe_quantize_rows_fp4" else ("src", "scale", "rows", "cols", "dst")
+    assert getattr(L, fn)(*[a[n] for n in order], None) == code
+
+
+@pytest.mark.parametrize("fn,change,code", [
+    (fn, c, code) for fn in ("moe_quantize_weights_fp4", "moe_dequantize_weights_fp4") for c, code in (
+        (dict(w=None), ARG), (dict(wq=None), ARG), (dict(scale=None), ARG), (dict(E=0), ARG), (dict(E=70000), ARG), (dict(K=-32), ARG), (dict(N=0), ARG),
+        (dict(K=40), SHAPE), (dict(N=12), SHAPE), (dict(w=P + 8), ALIGN), (dict(wq=P + 4), ALIGN), (dict(scale=P + 8), ALIGN))
+], ids=str)
+def test_weights_fp4_refuse(L, fn, change, code):
+    a = dict(w=P, wq=P, scale=P, E=2, K=64, N=64) | change
+    order = ("w", "E", "K", "N", "wq", "scale") if fn == "moe_quantize_weights_fp4" else ("wq", "scale", "E", "K", "N", "w")
+    assert getattr(L, fn)(*[a[n] for n in order], None) == code
+
+
+def test_fp4_scale_bytes(L):
+    assert B.moe_fp4_scale_bytes(1, 32, 8) == 1024
+    for E, K, N in ((3, 4096, 1536), (2, 288, 136), (5, 2880, 2880)):
+        assert B.moe_fp4_scale_bytes(E, K, N) == Q.scale_bytes(E, K, N)
+    out = ctypes.c_size_t(0)
+    assert L.moe_fp4_scale_bytes(0, 32, 8, ctypes.byref(out)) == ARG and L.moe_fp4_scale_bytes(1, 32, 8, None) == ARG
+
+
+def shape(**kw):
+    a = dict(T=16, d=64, f=96, E=4, k=2, G=2, score_fn=0, flags=0) | kw
+    return B.MoEShape(*a.values())
+
+
+def layout(ptr=P):
+    return B.MoELayoutC(*[ptr] * 9)
+
+
+BAD_FLAGS = [B.MOE_FLAG_FUSED_FFN, B.MOE_FLAG_COMBINE_IN_EPILOGUE, B.MOE_FLAG_GEMM1_PAIR, B.MOE_FLAG_GEMM1_GATHER, B.MOE_FLAG_GEMM2_PAIR,
+             B.MOE_FLAG_GEMM2_SINGLE, B.MOE_FLAG_FUSED_FFN | B.MOE_FLAG_TRACK_DISPATCH]
+
+
+@pytest.mark.parametrize("kw,change,code", [
+    (dict(d=48), {}, SHAPE), (dict(f=80), {}, SHAPE), (dict(E=3), {}, ARG), *[(dict(flags=f), {}, ARG) for f in BAD_FLAGS],
+    *[({}, {n: None}, ARG) for n in ("xq", "sx", "w", "w1", "s1", "w3", "s3", "w2", "s2", "o", "ws")],
+    *[({}, {n: P + 64}, ALIGN) for n in ("xq", "w1", "w3", "w2", "o", "ws")], *[({}, {n: P + 8}, ALIGN) for n in ("w", "s1", "s3", "s2")],
+    ({}, dict(bytes=1000), SMALL),
+], ids=str)
+def test_expert_ffn_fp4_refuses(L, kw, change, code):
+    a = dict(xq=P, sx=P, lay=ctypes.byref(layout()), w=P, w1=P, s1=P, w3=P, s3=P, w2=P, s2=P, o=P, ws=P, bytes=1 << 30) | change
+    assert L.moe_expert_ffn_fp4(ctypes.byref(shape(**kw)), *a.values(), None) == code
+
+
+def test_expert_ffn_fp4_refuses_layouts(L):
+    args = (P, P, P, P, P, P, P, P, P, P, 1 << 30, None)
+    assert L.moe_expert_ffn_fp4(ctypes.byref(shape()), P, P, None, *args[1:]) == ARG
+    assert L.moe_expert_ffn_fp4(ctypes.byref(shape()), P, P, ctypes.byref(layout(P + 4)), *args[1:]) == ALIGN
+    assert L.moe_expert_ffn_fp4(None, P, P, ctypes.byref(layout()), *args[1:]) == ARG
+
+
+@pytest.mark.parametrize("kw,change,code", [
+    (dict(d=48), {}, SHAPE), (dict(f=80), {}, SHAPE), *[(dict(flags=f), {}, ARG) for f in BAD_FLAGS], (dict(flags=B.MOE_FLAG_SPARSE_TOPK), {}, ARG),
+    *[({}, {n: None}, ARG) for n in ("x", "wg", "w1", "s1", "w3", "s3", "w2", "s2", "y", "ws")],
+    *[({}, {n: P + 64}, ALIGN) for n in ("x", "w1", "w3", "w2", "y", "ws")], *[({}, {n: P + 8}, ALIGN) for n in ("wg", "s1", "s3", "s2", "logits")],
+    ({}, dict(bytes=1000), SMALL), ({}, dict(bias=P, stride=3), ARG),
+], ids=str)
+def test_layer_fp4_refuses(L, kw, change, code):
+    a = dict(x=P, wg=P, bias=None, stride=0, w1=P, s1=P, w3=P, s3=P, w2=P, s2=P, y=P, logits=None, idx=None, w=None, lay=None, ws=P, bytes=1 << 30) | change
+    assert L.moe_layer_fp4(ctypes.byref(shape(**kw)), *a.values(), None) == code
+
+
+@pytest.mark.skipif(not NO_GPU, reason="what is said without a device")
+def test_no_device_is_an_error(L):
+    lay = ctypes.byref(layout())
+    assert L.moe_rmsnorm(P, None, P, 0, 1e-6, 4, 64, None, P, None, None, None, None) == CUDA
+    assert L.moe_rmsnorm_backward(P, None, P, P, 0, P, 4, 64, P, P, P, 1024, None) == CUDA
+    assert L.moe_quantize_rows_fp4(P, 4, 64, P, P, None) == CUDA
+    assert L.moe_dequantize_rows_fp4(P, P, 4, 64, P, None) == CUDA
+    assert L.moe_quantize_weights_fp4(P, 1, 64, 64, P, P, None) == CUDA
+    assert L.moe_dequantize_weights_fp4(P, P, 1, 64, 64, P, None) == CUDA
+    assert L.moe_expert_ffn_fp4(ctypes.byref(shape()), P, P, lay, P, P, P, P, P, P, P, P, P, 1 << 30, None) == CUDA
+    assert L.moe_layer_fp4(ctypes.byref(shape()), P, P, None, 0, P, P, P, P, P, P, P, None, None, None, None, P, 1 << 30, None) == CUDA
+
+
+# ---- the oracles ------------------------------------------------------------------------------------------------------------
+def test_fp4_codes_against_search():
+    """Nearest element by search over all sixteen, ties to the even code; the block's exponent from its largest value."""
+    rng = np.random.default_rng(1)
+    v = np.concatenate([rng.standard_normal((200, 32)) * np.exp2(rng.integers(-20, 20, (200, 1))), np.tile(Q.BORDER, (1, 5))[:, :32]])
+    ex = Q.exponents(v)[:, 0]
+    codes = Q.codes_of(v, Q.exponents(v))
+    for row, e, c in zip(v, ex, codes):
+        assert 4 <= np.abs(row).max() / 2.0 ** e < 8
+        for x, got in zip(row / 2.0 ** e, c):
+            x = np.clip(x, -6, 6)
+            dist = np.abs(Q.GRID - abs(x))
+            best = np.flatnonzero(dist == dist.min())
+            want = best[best % 2 == 0][0] if best.size > 1 else best[0]
+            assert (got & 7) == want and bool(got & 8) == bool(np.signbit(x))
+
+
+def test_fp4_exact_values_survive_and_scales_have_their_places():
+    grid = np.concatenate([Q.GRID, -Q.GRID, Q.GRID, Q.GRID])[None, :] * 2.0 ** np.array([[-9], [0], [7]])
+    packed, scale = Q.quantize_rows(grid)
+    assert np.array_equal(Q.dequantize_rows(packed, scale), grid) and scale[:, 0].tolist() == [118, 127, 134]
+    s = np.arange(2 * 136 * 9, dtype=np.int64).reshape(2, 136, 9) % 251
+    tiles = Q.tile_scales(s.astype(np.uint8))
+    assert tiles.size == 2 * 2 * 2 * 1024
+    assert tiles[0] == s[0, 0, 0] and tiles[1] == s[0, 0, 1] and tiles[4] == s[0, 32, 0] and tiles[16] == s[0, 1, 0]
+    assert tiles[512] == s[0, 0, 4] and tiles[1024] == s[0, 0, 8] and tiles[1025] == 127 and tiles[2048] == s[0, 128, 0]
+    assert tiles[4096] == s[1, 0, 0]
+    assert Q.quantize_rows(np.zeros((1, 32)))[1][0, 0] == 127 and Q.quantize_rows(np.full((1, 32), 2.0 ** -133))[1][0, 0] == 0
+
+
+def test_norm_oracle_against_differences():
+    rng = np.random.default_rng(2)
+    x, r, w, c = rng.standard_normal((3, 24)), rng.standard_normal((3, 24)), rng.standard_normal(24), rng.standard_normal((3, 24))
+    s, rstd, y = N.rmsnorm(x, r, w, 0.1)
+    assert np.allclose((y / w / s) ** -2, (s * s).mean(1, keepdims=True) + 0.1)
+    dx, dw = N.rmsnorm_backward(c, s, w, rstd, r)
+    h = 1e-6
+    for i, j in ((0, 0), (1, 9), (2, 23)):
+        d = np.zeros_like(x)
+        d[i, j] = h
+        num = ((c * (N.rmsnorm(x + d, r, w, 0.1)[2] - N.rmsnorm(x - d, r, w, 0.1)[2])).sum()) / (2 * h) + r[i, j]
+        assert abs(num - dx[i, j]) < 1e-7
+        d = np.zeros_like(w)
+        d[j] = h
+        assert abs((c * (N.rmsnorm(x, r, w + d, 0.1)[2] - N.rmsnorm(x, r, w - d, 0.1)[2])).sum() / (2 * h) - dw[j]) < 1e-7
