@@ -92,8 +92,8 @@ WsPlan plan(const moe_shape_t& s) {
   p.row_src = take(P * 4);
   // FP4 form: scale chunks of the row tiles of x and of h (the sorted codes of x lie in `o`, those of h in `h`)
   const bool fp4 = s.d % 32 == 0 && s.f % 32 == 0;
-  p.sf_x = take(fp4 ? fp4_scale_bytes((size_t)fp4_row_tiles(to_shape(s)), s.d) : 0);
-  p.sf_h = take(fp4 ? fp4_scale_bytes((size_t)fp4_row_tiles(to_shape(s)), s.f) : 0);
+  p.sf_x = take(fp4 ? fp4_scale_bytes((size_t)fp4_row_sets(to_shape(s)), s.d) : 0);
+  p.sf_h = take(fp4 ? fp4_scale_bytes((size_t)fp4_row_sets(to_shape(s)), s.f) : 0);
   p.total = off;
   return p;
 }
@@ -808,7 +808,7 @@ int check_fp4(const moe_shape_t* s, const void* w1q, const void* s1, const void*
 }
 Fp4Args fp4_args(void* ws, const WsPlan& p, const void* sx, const void* s1, const void* s3, const void* s2) {
   return Fp4Args{static_cast<const uint8_t*>(sx), static_cast<const uint8_t*>(s1), static_cast<const uint8_t*>(s3),
-                 static_cast<const uint8_t*>(s2), at<uint8_t>(ws, p.sf_x), at<uint8_t>(ws, p.sf_h)};
+                 static_cast<const uint8_t*>(s2), at<uint8_t>(ws, p.sf_x), at<uint8_t>(ws, p.sf_h), at<float>(ws, p.sh)};
 }
 }  // namespace
 }  // namespace tcmoe

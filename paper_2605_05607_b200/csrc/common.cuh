@@ -249,8 +249,9 @@ struct Fp4Args {
   const uint8_t* sx;            // [a_rows, d / 32]
   const uint8_t *s1, *s3, *s2;  // scale chunks of the weights
   uint8_t *sfx, *sfh;           // scratch: scale chunks of the row tiles of x and of h
+  float* row_w;                 // scratch: gate weights in the order of the rows [P]
 };
-long long fp4_row_tiles(const Shape& s);   // row tiles at most
+long long fp4_row_sets(const Shape& s);   // sets of scale chunks of 128 rows, at most
 cudaError_t launch_expert_ffn_fp4(const Shape& s, const FfnArgs& a, const Fp4Args& q, cudaStream_t st);
 // ep.cu: the two steps that expert parallelism across GPUs adds to the single-GPU path
 cudaError_t launch_ep_pack(const Shape& s, const int32_t* topk_idx, const float* topk_w, const Layout& L,

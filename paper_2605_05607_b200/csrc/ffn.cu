@@ -30,11 +30,11 @@ EncodeTiledFn encode_fn() {
 // workspace regions), so the most recent ones are kept, keyed by exactly those arguments.
 struct MapKey {
   const void* base;
-  int bytes, rank;
+  int element, rank;
   cuuint64_t dims[3], strides[2];
   cuuint32_t box[3];
   bool operator==(const MapKey& o) const {
-    return base == o.base && bytes == o.bytes && rank == o.rank && dims[0] == o.dims[0] && dims[1] == o.dims[1] &&
+    return base == o.base && element == o.element && rank == o.rank && dims[0] == o.dims[0] && dims[1] == o.dims[1] &&
            dims[2] == o.dims[2] && strides[0] == o.strides[0] && strides[1] == o.strides[1] && box[0] == o.box[0] &&
            box[1] == o.box[1] && box[2] == o.box[2];
   }
@@ -50,13 +50,13 @@ int g_map_count = 0, g_map_next = 0;   // entries in use, next slot to overwrite
 
 }  // namespace
 
-// Every map of this library: bf16 (bytes = 0) or one-byte (bytes = 1) elements, 128-byte swizzle, no interleave,
+// Every map of this library: bf16 or one-byte elements with 128-byte swizzle, or 32-bit words (of scale chunks) without; no interleave,
 // 256-byte L2 promotion, zero fill outside the tensor.
-bool encode_tiled(CUtensorMap* map, bool bytes, int rank, const void* base, const cuuint64_t* dims,
+bool encode_tiled(CUtensorMap* map, int element, int rank, const void* base, const cuuint64_t* dims,
                   const cuuint64_t* strides, const cuuint32_t* box) {
   MapKey key{};
   key.base = base;
-  key.bytes = bytes ? 1 : 0;
+  key.element = element;
   key.rank = rank;
   for (int i = 0; i < rank; ++i) { key.dims[i] = dims[i]; key.box[i] = box[i]; }
   for (int i = 0; i + 1 < rank; ++i) key.strides[i] = strides[i];
@@ -68,9 +68,9 @@ bool encode_tiled(CUtensorMap* map, bool bytes, int rank, const void* base, cons
   EncodeTiledFn fn = encode_fn();
   if (fn == nullptr) return false;
   const cuuint32_t estr[3] = {1, 1, 1};
-  if (fn(map, bytes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank,
-         const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+  const CUtensorMapDataType types[3] = {CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, CU_TENSOR_MAP_DATA_TYPE_UINT8, CU_TENSOR_MAP_DATA_TYPE_UINT32};
+  if (fn(map, types[element], (cuuint32_t)rank, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+         element == MAP_WORDS ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
     return false;
   std::lock_guard<std::mutex> lock(g_map_mutex);
   MapEntry& e = g_map_cache[g_map_next];
@@ -92,7 +92,7 @@ bool make_weight_map(CUtensorMap* map, const void* base, int E, int K, int N) {
   cuuint64_t dims[3] = {(cuuint64_t)N, (cuuint64_t)K, (cuuint64_t)E};
   cuuint64_t strides[2] = {(cuuint64_t)N * 2, (cuuint64_t)N * K * 2};
   cuuint32_t box[3] = {64, BK, 1};
-  return encode_tiled(map, false, 3, base, dims, strides, box);
+  return encode_tiled(map, MAP_BF16, 3, base, dims, strides, box);
 }
 
 // activations [rows, K] row-major, bf16 or E4M3: box = 128 bytes of K x box_rows rows
@@ -100,7 +100,7 @@ bool make_act_map(CUtensorMap* map, const void* base, long long rows, int K, boo
   cuuint64_t dims[2] = {(cuuint64_t)K, (cuuint64_t)rows};
   cuuint64_t strides[1] = {(cuuint64_t)K * (fp8 ? 1 : 2)};
   cuuint32_t box[2] = {fp8 ? 128u : (cuuint32_t)BK, (cuuint32_t)box_rows};
-  return encode_tiled(map, fp8, 2, base, dims, strides, box);
+  return encode_tiled(map, fp8 ? MAP_BYTES : MAP_BF16, 2, base, dims, strides, box);
 }
 
 // E4M3 weights [E, N, K] (K contiguous): box = 128 bytes of K x box_cols output columns x 1, 128-byte swizzle
@@ -108,7 +108,7 @@ bool make_weight_map_fp8(CUtensorMap* map, const void* base, int E, int N, int K
   cuuint64_t dims[3] = {(cuuint64_t)K, (cuuint64_t)N, (cuuint64_t)E};
   cuuint64_t strides[2] = {(cuuint64_t)K, (cuuint64_t)N * K};
   cuuint32_t box[3] = {128, (cuuint32_t)box_cols, 1};
-  return encode_tiled(map, true, 3, base, dims, strides, box);
+  return encode_tiled(map, MAP_BYTES, 3, base, dims, strides, box);
 }
 
 // bf16 weights [E, K, N] read as the TRANSPOSED operand of a backward GEMM: the same memory seen as [E, N' = K, K' = N]
@@ -117,7 +117,7 @@ bool make_weight_map_kmajor(CUtensorMap* map, const void* base, int E, int rows,
   cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)E};
   cuuint64_t strides[2] = {(cuuint64_t)cols * 2, (cuuint64_t)rows * cols * 2};
   cuuint32_t box[3] = {64, 128, 1};
-  return encode_tiled(map, false, 3, base, dims, strides, box);
+  return encode_tiled(map, MAP_BF16, 3, base, dims, strides, box);
 }
 
 // bf16 rows [rows, cols] read with the row index as K (weight gradients): box = 64 columns x 64 rows
@@ -125,7 +125,15 @@ bool make_rows_map_mn(CUtensorMap* map, const void* base, long long rows, int co
   cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
   cuuint64_t strides[1] = {(cuuint64_t)cols * 2};
   cuuint32_t box[2] = {64, 64};
-  return encode_tiled(map, false, 2, base, dims, strides, box);
+  return encode_tiled(map, MAP_BF16, 2, base, dims, strides, box);
+}
+
+// scale chunks of 512 bytes: box = the two of a pipeline stage
+bool make_scale_map(CUtensorMap* map, const void* base, long long chunks) {
+  cuuint64_t dims[2] = {128, (cuuint64_t)chunks};
+  cuuint64_t strides[1] = {512};
+  cuuint32_t box[2] = {128, 2};
+  return encode_tiled(map, MAP_WORDS, 2, base, dims, strides, box);
 }
 
 // bf16 [E, rows, cols] as the target of TMA stores: box = 64 columns x 128 rows x 1
@@ -133,7 +141,7 @@ bool make_store_map(CUtensorMap* map, const void* base, int E, int rows, int col
   cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)E};
   cuuint64_t strides[2] = {(cuuint64_t)cols * 2, (cuuint64_t)cols * rows * 2};
   cuuint32_t box[3] = {64, BM, 1};
-  return encode_tiled(map, false, 3, base, dims, strides, box);
+  return encode_tiled(map, MAP_BF16, 3, base, dims, strides, box);
 }
 
 }  // namespace ffn

@@ -164,7 +164,8 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
 
 // tensor maps (ffn.cu).  encode_tiled is the one place that calls cuTensorMapEncodeTiled; it keeps the most recent maps,
 // keyed by every argument of the encode, and clear_map_cache forgets them.
-bool encode_tiled(CUtensorMap* map, bool bytes, int rank, const void* base, const cuuint64_t* dims,
+enum { MAP_BF16 = 0, MAP_BYTES = 1, MAP_WORDS = 2 };   // elements of a map
+bool encode_tiled(CUtensorMap* map, int element, int rank, const void* base, const cuuint64_t* dims,
                   const cuuint64_t* strides, const cuuint32_t* box);
 void clear_map_cache();
 bool make_weight_map(CUtensorMap* map, const void* base, int E, int K, int N);
@@ -172,6 +173,7 @@ bool make_act_map(CUtensorMap* map, const void* base, long long rows, int K, boo
 bool make_weight_map_fp8(CUtensorMap* map, const void* base, int E, int N, int K, int box_cols = 128);
 bool make_weight_map_kmajor(CUtensorMap* map, const void* base, int E, int rows, int cols);
 bool make_rows_map_mn(CUtensorMap* map, const void* base, long long rows, int cols);
+bool make_scale_map(CUtensorMap* map, const void* base, long long chunks);
 bool make_store_map(CUtensorMap* map, const void* base, int E, int rows, int cols);
 cudaError_t launch_wgrad_pair(const CUtensorMap& m_a, const CUtensorMap& m_b, const int32_t* poff, long long rows_total, void* dw, int E,
                               int M, int N, int32_t* status, cudaStream_t st);

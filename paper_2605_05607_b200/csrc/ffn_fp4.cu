@@ -13,7 +13,6 @@
 //
 // TMEM: two accumulator buffers of 2 x 96 columns, then 24 columns of scales per stage.  Warp roles: 0-7 epilogue, 8 TMA, 9 UMMA and TMEM
 // owner.  One persistent CTA per SM; every wait is bounded.
-#include "ffn_common.cuh"
 #include "ffn_fp4.cuh"
 
 #include <atomic>
@@ -22,10 +21,9 @@ namespace tcmoe {
 namespace ffn {
 namespace {
 
-constexpr int F4_BK = 256;                          // K per stage
 constexpr int W_BYTES = 128 * 128;                  // one half of the weight tile: 128 columns x 256 of K
 constexpr int X_BYTES = 128 * F4_ROWS;              // the tile's rows
-constexpr int SF_BYTES = 1024;                      // scales of 128 rows x 256 of K
+constexpr int SF_BYTES = F4_SF_BYTES;
 constexpr int STAGE_BYTES = 2 * W_BYTES + X_BYTES + 3 * SF_BYTES;   // W W X sfX sfW sfW
 constexpr int NSTAGE = 4;
 constexpr int SF_COLS = 24;                         // TMEM columns of a stage's scales
@@ -37,45 +35,9 @@ constexpr int NUM_BARS = 2 * NSTAGE + 4;
 constexpr int EPI_WARPS = 8, TMA_WARP = EPI_WARPS, MMA_WARP = EPI_WARPS + 1;
 constexpr int THREADS = (EPI_WARPS + 2) * 32;
 constexpr int TABLE_BYTES = (2 * (MAX_E + 1) * 4 + 15) & ~15;
-constexpr int SMEM_BYTES = 1024 + NSTAGE * STAGE_BYTES + NUM_BARS * 8 + 64 + TABLE_BYTES;
+constexpr int SMEM_BYTES = 1024 + NSTAGE * STAGE_BYTES + NUM_BARS * 8 + 64 + TABLE_BYTES + EPI_WARPS * F4Out<F4_ROWS>::BYTES;
 static_assert(SMEM_BYTES <= 232448, "shared memory of an SM");
 constexpr uint32_t HINT = 1000;
-
-// Instruction descriptor of kind::mxf4: A, B E2M1, both K-major, scales E8M0, M = 128 (weights), N = n rows; the scale pair of an
-// instruction's 64 of K is bytes id, id + 1 of the columns.
-__host__ __device__ constexpr uint32_t idesc_f4(int n, int id) {
-  return ((uint32_t)id << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | (1u << 23) | ((uint32_t)(128 >> 7) << 27) |
-         ((uint32_t)id << 29);
-}
-// 32 rows of 16 bytes in shared memory, no swizzle: eight-row groups 128 bytes apart
-__device__ __forceinline__ uint64_t scale_desc(uint32_t smem_addr) {
-  return (uint64_t)((smem_addr & 0x3FFFF) >> 4) | ((uint64_t)(128 >> 4) << 16) | ((uint64_t)(128 >> 4) << 32) | (1ull << 46);
-}
-
-// Tiles of F4_ROWS rows per expert, exclusive prefix, by the first warp of the block (tp[E] = all of them).
-__device__ __forceinline__ void tile_table(const int32_t* expert_offsets, int E, int* tp, int* eoff, int lane) {
-  int base = 0;
-  for (int e0 = 0; e0 < E; e0 += 32) {
-    const int e = e0 + lane;
-    const int lo = __ldcg(expert_offsets + min(e, E)), hi = __ldcg(expert_offsets + min(e + 1, E));
-    const int tiles = (hi - lo + F4_ROWS - 1) / F4_ROWS;
-    int sum = tiles;
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-      const int u = __shfl_up_sync(0xFFFFFFFFu, sum, off);
-      if (lane >= off) sum += u;
-    }
-    if (e < E) {
-      tp[e] = base + sum - tiles;
-      eoff[e] = lo;
-      if (e == E - 1) {
-        tp[E] = base + sum;
-        eoff[E] = hi;
-      }
-    }
-    base += __shfl_sync(0xFFFFFFFFu, sum, 31);
-  }
-}
 
 struct F4Tile {
   int e, mt, row0, rows, c0, halves;   // expert, row tile over all experts, first row, rows; first 128-column chunk, halves in use
@@ -119,7 +81,7 @@ ffn_fp4_kernel(const __grid_constant__ CUtensorMap map_wa, const __grid_constant
     ptx::tmem_relinquish();
   }
   grid_dependency_sync();   // nothing above touches global data
-  if (warp == 0) tile_table(p.expert_offsets, p.E, tp_s, eoff_s, lane);
+  if (warp == 0) f4_tile_table(p.expert_offsets, p.E, F4_ROWS, tp_s, eoff_s, lane);
   if (threadIdx.x == 32) *abort_s = p.status[ST_ABORT];
   ptx::tc_fence_before();
   __syncthreads();
@@ -136,36 +98,42 @@ ffn_fp4_kernel(const __grid_constant__ CUtensorMap map_wa, const __grid_constant
     *abort_flag = 1;
   };
   // expert by expert, and inside one column tile by column tile, rows fastest: CTAs that run together share weights in L2
-  auto tile_of = [&](int w) {
-    int lo = 0, hi = p.E;   // tp[lo] * n_tiles <= w < tp[hi] * n_tiles
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (tp_s[mid] * n_tiles <= w) lo = mid; else hi = mid;
-    }
-    const int local = w - tp_s[lo] * n_tiles, mts = tp_s[lo + 1] - tp_s[lo];
+  auto tile_of = [&](int w, int from) {   // from: an expert at or before the tile's
+    const int lo = f4_expert_from(tp_s, from, n_tiles, w);
+    const uint32_t local = (uint32_t)(w - tp_s[lo] * n_tiles), mts = (uint32_t)(tp_s[lo + 1] - tp_s[lo]), c = local / mts;
     F4Tile t;
     t.e = lo;
-    const int m = local % mts;
+    const int m = (int)(local - c * mts);
     t.mt = tp_s[lo] + m;
     t.row0 = eoff_s[lo] + m * F4_ROWS;
     t.rows = min(F4_ROWS, eoff_s[lo + 1] - t.row0);
-    const int c = local / mts;
-    t.c0 = GLU ? c : 2 * c;
+    t.c0 = GLU ? (int)c : 2 * (int)c;
     t.halves = GLU ? 2 : min(2, p.NC - t.c0);
     return t;
   };
 
   if (warp < EPI_WARPS) {
     // ================================ epilogue: lane = column, TMEM column = row ================================
-    const int quarter = warp & 3, turn = warp >> 2, odd = lane & 1;
+    const int quarter = warp & 3, turn = warp >> 2;
+    const uint32_t out_mem = ptx::smem_u32(tp_s) + TABLE_BYTES + (uint32_t)(warp * F4Out<F4_ROWS>::BYTES);   // GEMM-2
     int tl = 0;
+    F4Tile t{}, next{};
+    float rw[(F4Out<F4_ROWS>::TURNS + 1) / 2];
+    if ((int)blockIdx.x < total) {
+      next = tile_of(blockIdx.x, 0);
+      if (!GLU) f4_fetch_weights<F4_ROWS>(p, next.row0, next.rows, turn, lane, rw);
+    }
     for (int w = blockIdx.x; w < total && !*abort_flag; w += gridDim.x, ++tl) {
-      const F4Tile t = tile_of(w);
+      t = next;
+      if (!GLU) f4_keep_weights<F4_ROWS>(rw, out_mem, lane);
+      if (w + (int)gridDim.x < total) {
+        next = tile_of(w + gridDim.x, t.e);
+        if (!GLU) f4_fetch_weights<F4_ROWS>(p, next.row0, next.rows, turn, lane, rw);
+      }
       const int buf = tl & 1;
       if (!ptx::mbar_wait_warp<true>(tfull_bar(buf), (tl >> 1) & 1, abort_flag, global_abort)) { timeout(1); break; }
       ptx::tc_fence_after();
       const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * BUF_COLS);
-      const int c = quarter * 32 + lane;
 #pragma unroll 1
       for (int r0 = turn * 16; r0 < t.rows; r0 += 32) {   // the two warps of a quarter take turns
         uint32_t a[16], b[16];
@@ -199,22 +167,9 @@ ffn_fp4_kernel(const __grid_constant__ CUtensorMap map_wa, const __grid_constant
             }
           }
         } else {
-          const int mine = r0 + (lane & 15);
-          float rs = 1.f;   // gate weight of this lane's row of the 16
-          if (mine < t.rows && p.topk_w != nullptr) rs = __ldg(p.topk_w + __ldg(p.row_pair + t.row0 + mine));
-          // two rows at a time: neighbouring lanes swap, and each stores two columns of one of the rows
-          auto put = [&](float v0, float v1, int r, int col) {
-            const float got = __shfl_xor_sync(0xFFFFFFFFu, odd ? v0 : v1, 1);
-            const int row = r0 + r + odd, at = col - odd;
-            if (row < t.rows && at < p.N)
-              *reinterpret_cast<uint32_t*>(p.out + (size_t)(t.row0 + row) * (size_t)p.N + at) = odd ? pack2(got, v1) : pack2(v0, got);
-          };
-#pragma unroll
-          for (int r = 0; r < 16; r += 2) {
-            const float w0 = __shfl_sync(0xFFFFFFFFu, rs, r), w1 = __shfl_sync(0xFFFFFFFFu, rs, r + 1);
-            put(w0 * __uint_as_float(a[r]), w1 * __uint_as_float(a[r + 1]), r, t.c0 * 128 + c);
-            if (t.halves > 1) put(w0 * __uint_as_float(b[r]), w1 * __uint_as_float(b[r + 1]), r, t.c0 * 128 + 128 + c);
-          }
+          const int col0 = t.c0 * 128 + quarter * 32;
+          f4_store_rows<F4_ROWS>(p, a, out_mem, r0 >> 5, lane, t.row0 + r0, t.rows - r0, col0);
+          if (t.halves > 1) f4_store_rows<F4_ROWS>(p, b, out_mem, r0 >> 5, lane, t.row0 + r0, t.rows - r0, col0 + 128);
         }
       }
       ptx::tc_fence_before();
@@ -225,8 +180,10 @@ ffn_fp4_kernel(const __grid_constant__ CUtensorMap map_wa, const __grid_constant
     // ================================ TMA producer ================================
     if (lane == 0) {
       uint32_t it = 0;
+      int e = 0;
       for (int w = blockIdx.x; w < total && !*abort_flag; w += gridDim.x) {
-        const F4Tile t = tile_of(w);
+        const F4Tile t = tile_of(w, e);
+        e = t.e;
         const int box = (t.rows + 31) / 32;   // rows by 32; what the stage held behind them reaches no stored row
         const uint32_t bytes = (uint32_t)(t.halves * (W_BYTES + SF_BYTES) + box * 32 * 128 + SF_BYTES);
         const size_t wc0 = (size_t)t.e * p.NC + t.c0, wc1 = GLU ? wc0 : wc0 + 1;
@@ -256,17 +213,18 @@ ffn_fp4_kernel(const __grid_constant__ CUtensorMap map_wa, const __grid_constant
     const uint32_t base = __shfl_sync(0xFFFFFFFFu, smem_base, 0), tmem = __shfl_sync(0xFFFFFFFFu, tmem_base, 0);
     const uint64_t w_desc = desc_at(desc_base(16, 1024), base), x_desc = desc_at(desc_base(16, 1024), base + 2 * W_BYTES);
     const uint64_t sf_desc = scale_desc(base + 2 * W_BYTES + X_BYTES);
-    int s = 0, tl = 0;
+    int s = 0, tl = 0, e = 0;
     uint32_t ph = 0;
     bool ok = true;
     for (int w = blockIdx.x; ok && w < total && !*abort_flag; w += gridDim.x, ++tl) {
       const int buf = tl & 1;
-      const F4Tile t = tile_of(w);
+      const F4Tile t = tile_of(w, e);
+      e = t.e;
       if (!ptx::mbar_wait(tempty_bar(buf), ((tl >> 1) & 1) ^ 1, abort_flag, global_abort)) { timeout(3); break; }
       ptx::tc_fence_after();
       const uint32_t d = tmem + (uint32_t)(buf * BUF_COLS);
       const int n = (t.rows + 15) & ~15;
-      const uint32_t id0 = idesc_f4(n, 0), id1 = idesc_f4(n, 2);
+      const uint32_t id0 = idesc_f4(128, n, 0), id1 = idesc_f4(128, n, 2);
       for (int kb = 0; kb < KB; ++kb) {
         if (!ptx::mbar_wait(full_bar(s), ph, abort_flag, global_abort)) { timeout(4); ok = false; break; }
         ptx::tc_fence_after();
@@ -303,23 +261,25 @@ ffn_fp4_kernel(const __grid_constant__ CUtensorMap map_wa, const __grid_constant
   }
 }
 
-// Quantised rows, gathered into expert-sorted order, and their scales into the chunks of the row tiles.  A warp per row; which expert a row
+// Quantised rows, gathered into expert-sorted order, their scales into the chunks of the row tiles, and the rows' gate weights.  A warp per row; which expert a row
 // belongs to, and which tile of all, comes from one pass over the offsets.
 __global__ void __launch_bounds__(256) fp4_sort_kernel(const uint4* __restrict__ xq, const uint8_t* __restrict__ sx, int a_rows,
                                                        const int32_t* __restrict__ gather_idx, int gather_div,
-                                                       const int32_t* __restrict__ expert_offsets, int E, int K, int capacity, uint4* xs,
-                                                       uint8_t* sfx, int32_t* status) {
+                                                       const int32_t* __restrict__ expert_offsets, int E, int K, int capacity, int tile_rows, uint4* xs,
+                                                       uint8_t* sfx, const float* __restrict__ topk_w, const int32_t* __restrict__ row_pair, float* row_w,
+                                                       int32_t* status) {
   grid_dependency_sync();
   const int lane = threadIdx.x & 31;
   const int KB = K / 32, words = fp4::chunks(K);   // scale bytes of a row, and its 4-byte words in the chunks
   const int rows = min(__ldg(expert_offsets + E), capacity);
   for (int r = blockIdx.x * 8 + (threadIdx.x >> 5); r < rows; r += gridDim.x * 8) {
     int src = __ldg(gather_idx + r);
+    if (row_w != nullptr && lane == 0) row_w[r] = __ldg(topk_w + __ldg(row_pair + r));
     if (gather_div > 1) src /= gather_div;
     int before = 0, first = 0;   // tiles of the experts that end at or before this row; first row of its own
     for (int e = lane; e < E; e += 32) {
       const int lo = __ldg(expert_offsets + e), hi = __ldg(expert_offsets + e + 1);
-      if (hi <= r) before += (hi - lo + F4_ROWS - 1) / F4_ROWS;
+      if (hi <= r) before += (hi - lo + tile_rows - 1) / tile_rows;
       else if (lo <= r) first = lo;
     }
     before = __reduce_add_sync(0xFFFFFFFFu, before);
@@ -331,8 +291,7 @@ __global__ void __launch_bounds__(256) fp4_sort_kernel(const uint4* __restrict__
     const uint4* from = xq + (size_t)src * KB;
     uint4* to = xs + (size_t)r * KB;
     for (int v = lane; v < KB; v += 32) to[v] = __ldg(from + v);
-    const int mt = before + (r - first) / F4_ROWS, lr = (r - first) % F4_ROWS;
-    uint8_t* sf = sfx + (size_t)mt * words * 512 + (lr & 31) * 16 + (lr >> 5) * 4;
+    uint8_t* sf = sfx + f4_scale_at(before, r - first, tile_rows, words, 0);
     const uint8_t* s = sx + (size_t)src * KB;
     for (int c = lane; c < words; c += 32) {
       uint32_t v = 0;
@@ -355,7 +314,7 @@ cudaError_t launch_gemm(const F4Params& p, const void* wa, const void* wb, const
   CUtensorMap m_a, m_b;
   F4RowMaps x;
   if (!make_weight_map_fp8(&m_a, wa, p.E, p.N, p.K / 2, 128) || !make_weight_map_fp8(&m_b, wb, p.E, p.N, p.K / 2, 128)) return cudaErrorInvalidValue;
-  for (int i = 0; i < F4_ROWS / 32; ++i)
+  for (int i = 0; i < 4; ++i)
     if (!make_act_map(&x.m[i], rows, n_rows, p.K / 2, true, 32 * (i + 1))) return cudaErrorInvalidValue;
   ProfileScope prof(GLU ? KID_GEMM1 : KID_GEMM2, st);
   return launch_pdl(ffn_fp4_kernel<GLU>, dim3(sm_count()), dim3(THREADS), SMEM_BYTES, st, m_a, m_b, x, p);
@@ -364,17 +323,24 @@ cudaError_t launch_gemm(const F4Params& p, const void* wa, const void* wb, const
 }  // namespace
 }  // namespace ffn
 
-long long fp4_row_tiles(const Shape& s) {
-  const long long P = (long long)s.T * s.k;
-  return P / ffn::F4_ROWS + (s.E < P ? s.E : P);
+long long fp4_row_sets(const Shape& s) {
+  const long long P = (long long)s.T * s.k, e = s.E < P ? s.E : P;
+  const long long one = P / ffn::F4_ROWS + e, two = 2 * (P / ffn::F4_PAIR_ROWS2 + e);   // every expert's last tile may be a part
+  return one > two ? one : two;
 }
+
+static bool fp4_pairs(const Shape& s) { return (long long)s.T * s.k >= 256ll * s.E; }
 
 cudaError_t launch_expert_ffn_fp4(const Shape& s, const FfnArgs& a, const Fp4Args& q, cudaStream_t st) {
   if (s.T == 0) return cudaSuccess;
   const int P = s.T * s.k;
+  const bool pairs = fp4_pairs(s);
+  const int rows1 = pairs ? ffn::F4_PAIR_ROWS1 : ffn::F4_ROWS, rows2 = pairs ? ffn::F4_PAIR_ROWS2 : ffn::F4_ROWS;
+  float* row_w = a.topk_w != nullptr ? q.row_w : nullptr;
   const int blocks = (P + 7) / 8, cap = sm_count() * 8;
   cudaError_t e = launch_pdl(ffn::fp4_sort_kernel, dim3(blocks < cap ? blocks : cap), dim3(256), 0, st, static_cast<const uint4*>(a.a_src),
-                             q.sx, a.a_rows, a.gather_idx, a.gather_div, a.expert_offsets, s.E, s.d, P, static_cast<uint4*>(a.xs), q.sfx, a.status);
+                             q.sx, a.a_rows, a.gather_idx, a.gather_div, a.expert_offsets, s.E, s.d, P, rows1, static_cast<uint4*>(a.xs), q.sfx,
+                             a.topk_w, a.row_pair, row_w, a.status);
   if (e != cudaSuccess) return e;
   ffn::F4Params g1{};
   g1.expert_offsets = a.expert_offsets;
@@ -387,8 +353,10 @@ cudaError_t launch_expert_ffn_fp4(const Shape& s, const FfnArgs& a, const Fp4Arg
   g1.sfb = q.s3;
   g1.hq = static_cast<uint32_t*>(a.h);
   g1.sfh = q.sfh;
+  g1.h_rows = rows2;
   g1.status = a.status;
-  if ((e = ffn::launch_gemm<true>(g1, a.w1, a.w3, a.xs, P, st)) != cudaSuccess) return e;
+  e = pairs ? ffn::launch_fp4_pair(true, g1, a.w1, a.w3, a.xs, P, fp4_row_sets(s), st) : ffn::launch_gemm<true>(g1, a.w1, a.w3, a.xs, P, st);
+  if (e != cudaSuccess) return e;
   ffn::F4Params g2{};
   g2.expert_offsets = a.expert_offsets;
   g2.E = s.E;
@@ -398,10 +366,9 @@ cudaError_t launch_expert_ffn_fp4(const Shape& s, const FfnArgs& a, const Fp4Arg
   g2.sfx = q.sfh;
   g2.sfa = g2.sfb = q.s2;
   g2.out = static_cast<__nv_bfloat16*>(a.o);
-  g2.topk_w = a.topk_w;
-  g2.row_pair = a.row_pair;
+  g2.row_w = row_w;
   g2.status = a.status;
-  return ffn::launch_gemm<false>(g2, a.w2, a.w2, a.h, P, st);
+  return pairs ? ffn::launch_fp4_pair(false, g2, a.w2, a.w2, a.h, P, fp4_row_sets(s), st) : ffn::launch_gemm<false>(g2, a.w2, a.w2, a.h, P, st);
 }
 
 }  // namespace tcmoe

@@ -416,7 +416,7 @@ cudaError_t launch_gate_logits(const Shape& s, const void* x, const float* w_gat
     cuuint64_t dims[2] = {(cuuint64_t)s.d, (cuuint64_t)s.T};
     cuuint64_t strides[1] = {(cuuint64_t)s.d * 2};
     cuuint32_t box[2] = {BK, (cuuint32_t)a_rows};
-    if (!ffn::encode_tiled(&m_x, false, 2, x, dims, strides, box)) return cudaErrorInvalidValue;
+    if (!ffn::encode_tiled(&m_x, ffn::MAP_BF16, 2, x, dims, strides, box)) return cudaErrorInvalidValue;
   }
   ProfileScope prof(KID_GATE, st);
   if (plan.pre) {
@@ -424,7 +424,7 @@ cudaError_t launch_gate_logits(const Shape& s, const void* x, const float* w_gat
     cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)s.d, 3};
     cuuint64_t strides[2] = {(cuuint64_t)cols * 2, (cuuint64_t)cols * s.d * 2};
     cuuint32_t box[3] = {64, BK, 1};
-    if (!ffn::encode_tiled(&m_w, false, 3, wsplit, dims, strides, box)) return cudaErrorInvalidValue;
+    if (!ffn::encode_tiled(&m_w, ffn::MAP_BF16, 3, wsplit, dims, strides, box)) return cudaErrorInvalidValue;
     size_t blocks = ((size_t)s.d * cols + 255) / 256;
     if (blocks > (size_t)sm_count() * 8) blocks = (size_t)sm_count() * 8;
     cudaError_t err = launch_pdl(split_gate_kernel, (unsigned)blocks, 256, 0, st, w_gate, static_cast<__nv_bfloat16*>(wsplit), s.d,

@@ -162,6 +162,16 @@ def check_ffn(shape, ws, lay, xg, w, wt, weighted=True):
 SMALL = [(1,), (1, 0, 3), (16, 17), (33, 1, 95, 96), (97, 192, 193), (0, 0, 5), (300,), (31, 32, 64, 65, 128, 129)]
 
 
+LARGE = [(256,), (511,), (257, 300), (193, 700, 128), (1000, 0, 1, 600), (2600, 300), (385, 384, 383, 192, 320)]
+
+
+@pytest.mark.parametrize("counts", LARGE, ids=str)
+@pytest.mark.parametrize("d,f", [(32, 32), (256, 128), (288, 160), (512, 384), (96, 1056), (1056, 96)])
+def test_expert_ffn_fp4_of_many_rows_per_expert(counts, d, f):
+    shape, ws, lay, x, xg, idx, w, wt = routed(counts, d=d, f=f, seed=sum(counts) + d + f)
+    check_ffn(shape, ws, lay, xg, w, wt)
+
+
 @pytest.mark.parametrize("counts", SMALL, ids=str)
 @pytest.mark.parametrize("d,f", [(32, 32), (256, 128), (288, 160), (512, 384), (96, 1056), (1056, 96)])
 def test_expert_ffn_fp4_by_rows_per_expert(counts, d, f):
