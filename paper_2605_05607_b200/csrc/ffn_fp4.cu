@@ -81,7 +81,9 @@ ffn_fp4_kernel(const __grid_constant__ CUtensorMap map_wa, const __grid_constant
     ptx::tmem_relinquish();
   }
   grid_dependency_sync();   // nothing above touches global data
-  if (warp == 0) f4_tile_table(p.expert_offsets, p.E, F4_ROWS, tp_s, eoff_s, lane);
+  f4_load_offsets(p.expert_offsets, p.E, eoff_s);
+  __syncthreads();
+  if (warp == 0) f4_tile_table(eoff_s, p.E, F4_ROWS, tp_s, lane);
   if (threadIdx.x == 32) *abort_s = p.status[ST_ABORT];
   ptx::tc_fence_before();
   __syncthreads();
@@ -261,42 +263,62 @@ ffn_fp4_kernel(const __grid_constant__ CUtensorMap map_wa, const __grid_constant
   }
 }
 
-// Quantised rows, gathered into expert-sorted order, their scales into the chunks of the row tiles, and the rows' gate weights.  A warp per row; which expert a row
-// belongs to, and which tile of all, comes from one pass over the offsets.
+// Quantised rows, gathered into expert-sorted order, their scales into the chunks of the row tiles, and the rows' gate weights.  A warp takes `chunk`
+// neighbouring rows.  Only the scales need the tables of the experts, so those are built while the first rows are on their way.
 __global__ void __launch_bounds__(256) fp4_sort_kernel(const uint4* __restrict__ xq, const uint8_t* __restrict__ sx, int a_rows,
                                                        const int32_t* __restrict__ gather_idx, int gather_div,
-                                                       const int32_t* __restrict__ expert_offsets, int E, int K, int capacity, int tile_rows, uint4* xs,
-                                                       uint8_t* sfx, const float* __restrict__ topk_w, const int32_t* __restrict__ row_pair, float* row_w,
-                                                       int32_t* status) {
+                                                       const int32_t* __restrict__ expert_offsets, int E, int K, int capacity, int tile_rows,
+                                                       int chunk, uint4* xs, uint8_t* sfx, const float* __restrict__ topk_w,
+                                                       const int32_t* __restrict__ row_pair, float* row_w, int32_t* status) {
+  __shared__ int eoff[MAX_E + 1], tp[MAX_E + 1];
   grid_dependency_sync();
-  const int lane = threadIdx.x & 31;
-  const int KB = K / 32, words = fp4::chunks(K);   // scale bytes of a row, and its 4-byte words in the chunks
-  const int rows = min(__ldg(expert_offsets + E), capacity);
-  for (int r = blockIdx.x * 8 + (threadIdx.x >> 5); r < rows; r += gridDim.x * 8) {
-    int src = __ldg(gather_idx + r);
-    if (row_w != nullptr && lane == 0) row_w[r] = __ldg(topk_w + __ldg(row_pair + r));
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int KB = K / 32, words = fp4::chunks(K);              // scale bytes of a row, and its 4-byte words in the chunks
+  const long long r0 = ((long long)blockIdx.x * 8 + warp) * chunk;
+  const int n = (int)max(0ll, min((long long)chunk, min((long long)__ldg(expert_offsets + E), (long long)capacity) - r0));   // rows of this warp
+  f4_load_offsets(expert_offsets, E, eoff);
+  int src = -1;
+  if (lane < n) {
+    const int r = (int)r0 + lane;
+    src = __ldg(gather_idx + r);
     if (gather_div > 1) src /= gather_div;
-    int before = 0, first = 0;   // tiles of the experts that end at or before this row; first row of its own
-    for (int e = lane; e < E; e += 32) {
-      const int lo = __ldg(expert_offsets + e), hi = __ldg(expert_offsets + e + 1);
-      if (hi <= r) before += (hi - lo + tile_rows - 1) / tile_rows;
-      else if (lo <= r) first = lo;
-    }
-    before = __reduce_add_sync(0xFFFFFFFFu, before);
-    first = __reduce_max_sync(0xFFFFFFFFu, first);
     if (src < 0 || src >= a_rows) {
-      if (lane == 0) report_error(status, DEV_INDEX_OUT_OF_RANGE, KID_GEMM1, src, r);
-      continue;
+      report_error(status, DEV_INDEX_OUT_OF_RANGE, KID_GEMM1, src, r);
+      src = -1;
     }
-    const uint4* from = xq + (size_t)src * KB;
-    uint4* to = xs + (size_t)r * KB;
+    if (row_w != nullptr) row_w[r] = __ldg(topk_w + __ldg(row_pair + r));
+  }
+  for (int j = 0; j < n; ++j) {
+    const int s = __shfl_sync(0xFFFFFFFFu, src, j);
+    if (s < 0) continue;
+    const uint4* from = xq + (size_t)s * KB;
+    uint4* to = xs + (size_t)(r0 + j) * KB;
+#pragma unroll 4
     for (int v = lane; v < KB; v += 32) to[v] = __ldg(from + v);
-    uint8_t* sf = sfx + f4_scale_at(before, r - first, tile_rows, words, 0);
-    const uint8_t* s = sx + (size_t)src * KB;
+  }
+  __syncthreads();
+  if (warp == 0) f4_tile_table(eoff, E, tile_rows, tp, lane);
+  __syncthreads();
+  if (n == 0) return;
+  const bool whole = KB % 4 == 0 && (reinterpret_cast<uintptr_t>(sx) & 3) == 0;
+  int e = 0;
+  for (int hi = E; hi - e > 1;) {   // the first row's expert: the last that starts at or before it, and is not empty
+    const int mid = (e + hi) >> 1;
+    if (eoff[mid] <= (int)r0) e = mid; else hi = mid;
+  }
+  for (int j = 0; j < n; ++j) {
+    const int s = __shfl_sync(0xFFFFFFFFu, src, j), r = (int)r0 + j;
+    while (eoff[e + 1] <= r) ++e;
+    if (s < 0) continue;
+    uint8_t* sf = sfx + f4_scale_at(tp[e], r - eoff[e], tile_rows, words, 0);
+    const uint8_t* from = sx + (size_t)s * KB;
     for (int c = lane; c < words; c += 32) {
-      uint32_t v = 0;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v |= (4 * c + i < KB ? (uint32_t)__ldg(s + 4 * c + i) : 127u) << (8 * i);
+      uint32_t v = 0x7F7F7F7Fu;
+      if (4 * c < KB) {
+        if (whole) v = __ldg(reinterpret_cast<const uint32_t*>(from + 4 * c));
+        else
+          for (int i = 0; i < 4 && 4 * c + i < KB; ++i) v = (v & ~(0xFFu << (8 * i))) | ((uint32_t)__ldg(from + 4 * c + i) << (8 * i));
+      }
       *reinterpret_cast<uint32_t*>(sf + (size_t)c * 512) = v;
     }
   }
@@ -337,9 +359,9 @@ cudaError_t launch_expert_ffn_fp4(const Shape& s, const FfnArgs& a, const Fp4Arg
   const bool pairs = fp4_pairs(s);
   const int rows1 = pairs ? ffn::F4_PAIR_ROWS1 : ffn::F4_ROWS, rows2 = pairs ? ffn::F4_PAIR_ROWS2 : ffn::F4_ROWS;
   float* row_w = a.topk_w != nullptr ? q.row_w : nullptr;
-  const int blocks = (P + 7) / 8, cap = sm_count() * 8;
-  cudaError_t e = launch_pdl(ffn::fp4_sort_kernel, dim3(blocks < cap ? blocks : cap), dim3(256), 0, st, static_cast<const uint4*>(a.a_src),
-                             q.sx, a.a_rows, a.gather_idx, a.gather_div, a.expert_offsets, s.E, s.d, P, rows1, static_cast<uint4*>(a.xs), q.sfx,
+  const int chunk = P >= 8 * 64 * sm_count() ? 8 : 1;   // rows per warp: one as long as all of them are resident at once
+  cudaError_t e = launch_pdl(ffn::fp4_sort_kernel, dim3((unsigned)((P + 8 * chunk - 1) / (8 * chunk))), dim3(256), 0, st, static_cast<const uint4*>(a.a_src),
+                             q.sx, a.a_rows, a.gather_idx, a.gather_div, a.expert_offsets, s.E, s.d, P, rows1, chunk, static_cast<uint4*>(a.xs), q.sfx,
                              a.topk_w, a.row_pair, row_w, a.status);
   if (e != cudaSuccess) return e;
   ffn::F4Params g1{};

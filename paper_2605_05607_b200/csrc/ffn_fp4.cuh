@@ -46,29 +46,26 @@ __device__ __forceinline__ uint64_t scale_desc(uint32_t smem_addr) {
   return (uint64_t)((smem_addr & 0x3FFFF) >> 4) | ((uint64_t)(128 >> 4) << 16) | ((uint64_t)(128 >> 4) << 32) | (1ull << 46);
 }
 
-// Tiles of `rows` rows per expert, exclusive prefix (tp[E] = all of them), and the offsets (eoff, or NULL), by one warp.
-__device__ __forceinline__ void f4_tile_table(const int32_t* expert_offsets, int E, int rows, int* tp, int* eoff, int lane) {
+// Expert offsets into shared memory, by all threads of the block: one memory latency for any number of experts.  A barrier has to follow.
+__device__ __forceinline__ void f4_load_offsets(const int32_t* expert_offsets, int E, int* eoff) {
+  for (int i = threadIdx.x; i <= E; i += blockDim.x) eoff[i] = __ldcg(expert_offsets + i);
+}
+// Tiles of `rows` rows per expert, exclusive prefix (tp[E] = all of them), by one warp.
+__device__ __forceinline__ void f4_tile_table(const int* eoff, int E, int rows, int* tp, int lane) {
   int base = 0;
   for (int e0 = 0; e0 < E; e0 += 32) {
     const int e = e0 + lane;
-    const int lo = __ldcg(expert_offsets + min(e, E)), hi = __ldcg(expert_offsets + min(e + 1, E));
-    const int tiles = (hi - lo + rows - 1) / rows;
+    const int tiles = e < E ? (eoff[e + 1] - eoff[e] + rows - 1) / rows : 0;
     int sum = tiles;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
       const int u = __shfl_up_sync(0xFFFFFFFFu, sum, off);
       if (lane >= off) sum += u;
     }
-    if (e < E) {
-      tp[e] = base + sum - tiles;
-      if (eoff != nullptr) eoff[e] = lo;
-      if (e == E - 1) {
-        tp[E] = base + sum;
-        if (eoff != nullptr) eoff[E] = hi;
-      }
-    }
+    if (e < E) tp[e] = base + sum - tiles;
     base += __shfl_sync(0xFFFFFFFFu, sum, 31);
   }
+  if (lane == 0) tp[E] = base;
 }
 
 // The expert whose tiles hold task w (tp[e] * n_tiles <= w < tp[e + 1] * n_tiles), looked for from expert `e` on: a warp's tasks ascend, and a search

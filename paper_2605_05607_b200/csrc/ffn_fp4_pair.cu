@@ -90,8 +90,10 @@ ffn_fp4_pair_kernel(const __grid_constant__ CUtensorMap map_wa, const __grid_con
     ptx::tmem_relinquish_pair();
   }
   grid_dependency_sync();   // nothing above touches global data
-  if (warp == 0) f4_tile_table(p.expert_offsets, p.E, G::TILE_ROWS, tp_s, eoff_s, lane);
-  if (GLU && warp == 1) f4_tile_table(p.expert_offsets, p.E, p.h_rows, hp_s, nullptr, lane);
+  f4_load_offsets(p.expert_offsets, p.E, eoff_s);
+  __syncthreads();
+  if (warp == 0) f4_tile_table(eoff_s, p.E, G::TILE_ROWS, tp_s, lane);
+  if (GLU && warp == 1) f4_tile_table(eoff_s, p.E, p.h_rows, hp_s, lane);
   if (threadIdx.x == 64) *abort_s = p.status[ST_ABORT];
   ptx::tc_fence_before();
   __syncthreads();
