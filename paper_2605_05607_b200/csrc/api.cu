@@ -19,7 +19,7 @@ inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 // Regions of the workspace, in order.  Every region starts on a 1 KiB boundary.
 struct WsPlan {
   size_t status, emask, gmask, eprefix, gprefix, mt_prefix, mp_prefix, blk_start, blk_info, n_blocks, tracker, wsplit, xs, h, hq, sh, xq, sx, o, logits, topk_idx, topk_w;
-  size_t expert_counts, expert_offsets, group_counts, group_offsets, pair_row, row_pair, al, disp_token, row_src, sf_x, sf_h;
+  size_t expert_counts, expert_offsets, group_counts, group_offsets, pair_row, row_pair, al, disp_token, row_src, sf_x, sf_h, part4, arrived4;
   size_t total;
   int W;
 };
@@ -94,6 +94,8 @@ WsPlan plan(const moe_shape_t& s) {
   const bool fp4 = s.d % 32 == 0 && s.f % 32 == 0;
   p.sf_x = take(fp4 ? fp4_scale_bytes((size_t)fp4_row_sets(to_shape(s)), s.d) : 0);
   p.sf_h = take(fp4 ? fp4_scale_bytes((size_t)fp4_row_sets(to_shape(s)), s.f) : 0);
+  p.part4 = take(fp4 ? fp4_part_bytes(to_shape(s)) : 0);
+  p.arrived4 = take(fp4 ? fp4_arrived_bytes(to_shape(s)) : 0);
   p.total = off;
   return p;
 }
@@ -808,7 +810,8 @@ int check_fp4(const moe_shape_t* s, const void* w1q, const void* s1, const void*
 }
 Fp4Args fp4_args(void* ws, const WsPlan& p, const void* sx, const void* s1, const void* s3, const void* s2) {
   return Fp4Args{static_cast<const uint8_t*>(sx), static_cast<const uint8_t*>(s1), static_cast<const uint8_t*>(s3),
-                 static_cast<const uint8_t*>(s2), at<uint8_t>(ws, p.sf_x), at<uint8_t>(ws, p.sf_h), at<float>(ws, p.sh)};
+                 static_cast<const uint8_t*>(s2), at<uint8_t>(ws, p.sf_x), at<uint8_t>(ws, p.sf_h), at<float>(ws, p.sh),
+                 at<float>(ws, p.part4), at<int32_t>(ws, p.arrived4)};
 }
 }  // namespace
 }  // namespace tcmoe

@@ -250,7 +250,11 @@ struct Fp4Args {
   const uint8_t *s1, *s3, *s2;  // scale chunks of the weights
   uint8_t *sfx, *sfh;           // scratch: scale chunks of the row tiles of x and of h
   float* row_w;                 // scratch: gate weights in the order of the rows [P]
+  float* part;                  // scratch: parts of tiles that CTAs share, fp4_part_bytes
+  int32_t* arrived;             // scratch: fp4_arrived_bytes
 };
+size_t fp4_part_bytes(const Shape& s);
+size_t fp4_arrived_bytes(const Shape& s);
 long long fp4_row_sets(const Shape& s);   // sets of scale chunks of 128 rows, at most
 cudaError_t launch_expert_ffn_fp4(const Shape& s, const FfnArgs& a, const Fp4Args& q, cudaStream_t st);
 // ep.cu: the two steps that expert parallelism across GPUs adds to the single-GPU path

@@ -11,6 +11,13 @@
 // rows x 4 (512 bytes, by untiled bulk copies, in the layout that tcgen05.cp spreads over TMEM).  The scales' TMEM columns belong to the
 // stage: when a stage is filled again, the UMMAs that read its scales have completed.
 //
+// One persistent CTA per SM takes every 148th tile.  SHARE, for layers with fewer tiles than SMs: the stages of all tiles, one tile after the other, are
+// divided evenly among the CTAs.  A tile that several of them share leaves as fp32 parts; per epilogue warp, the one that writes the last part adds
+// them up, in the order of K whoever is last, puts the sums back into its accumulator and goes on as if they were its own.  GEMM-2 of one token,
+// top-2 of 4096 x 14336 (32 tiles): XXX us.  (With all layers divided this way, 64 tokens, top-8 of 128 experts of 4096 x 1536, took
+// 218 us instead of 211: neighbouring CTAs no longer stream neighbouring columns.  A form of its own, because the larger code alone costs the others
+// up to 4 us: instructions that are missed in the cache wait behind the weights that are on their way.)
+//
 // TMEM: two accumulator buffers of 2 x 96 columns, then 24 columns of scales per stage.  Warp roles: 0-7 epilogue, 8 TMA, 9 UMMA and TMEM
 // owner.  One persistent CTA per SM; every wait is bounded.
 #include "ffn_fp4.cuh"
@@ -43,7 +50,7 @@ struct F4Tile {
   int e, mt, row0, rows, c0, halves;   // expert, row tile over all experts, first row, rows; first 128-column chunk, halves in use
 };
 
-template <bool GLU>
+template <bool GLU, bool SHARE>
 __global__ void __launch_bounds__(THREADS, 1)
 ffn_fp4_kernel(const __grid_constant__ CUtensorMap map_wa, const __grid_constant__ CUtensorMap map_wb,
                const __grid_constant__ F4RowMaps xmaps, const F4Params p) {
@@ -90,8 +97,15 @@ ffn_fp4_kernel(const __grid_constant__ CUtensorMap map_wa, const __grid_constant
   ptx::tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
   const int n_tiles = GLU ? p.NC : (p.NC + 1) / 2;   // column tiles: one chunk of W1 and of W3, or two of W2
-  const int total = tp_s[p.E] * n_tiles;
   const int KB = (p.K + F4_BK - 1) / F4_BK;
+  // Items of this CTA: every gridDim.x-th tile, or (SHARE) the tiles that its share of the stages of all tiles lies in.
+  const int grid = (int)gridDim.x, total = tp_s[p.E] * n_tiles;
+  const int per = SHARE ? (total * KB + grid - 1) / grid : 0;
+  const int u0 = min(total * KB, (int)blockIdx.x * per), u1 = min(total * KB, u0 + per), w0 = SHARE ? u0 / KB : (int)blockIdx.x;
+  const int items = SHARE ? (u1 + KB - 1) / KB - w0 : (total - w0 + grid - 1) / grid;
+  auto tile_at = [&](int j) { return SHARE ? w0 + j : w0 + j * grid; };
+  auto kb_begin = [&](int j) { return SHARE ? max(0, u0 - (w0 + j) * KB) : 0; };
+  auto kb_end = [&](int j) { return SHARE ? min(KB, u1 - (w0 + j) * KB) : KB; };
   volatile int* abort_flag = abort_s;
   const volatile int* global_abort = p.status + ST_ABORT;
   auto timeout = [&](int detail) {
@@ -121,23 +135,74 @@ ffn_fp4_kernel(const __grid_constant__ CUtensorMap map_wa, const __grid_constant
     int tl = 0;
     F4Tile t{}, next{};
     float rw[(F4Out<F4_ROWS>::TURNS + 1) / 2];
-    if ((int)blockIdx.x < total) {
-      next = tile_of(blockIdx.x, 0);
+    // slot 2 i: the part of CTA i's first tile, which began before it; slot 2 i + 1: that of its last, which goes on behind it
+    auto slot = [&](int i, int r0) {
+      return p.part + ((size_t)i * p.part_rows + r0) * 256 + quarter * 32 + lane;   // per row: 128 columns of either half
+    };
+    if (items > 0) {
+      next = tile_of(tile_at(0), 0);
       if (!GLU) f4_fetch_weights<F4_ROWS>(p, next.row0, next.rows, turn, lane, rw);
     }
-    for (int w = blockIdx.x; w < total && !*abort_flag; w += gridDim.x, ++tl) {
+    for (; tl < items && !*abort_flag; ++tl) {
       t = next;
       if (!GLU) f4_keep_weights<F4_ROWS>(rw, out_mem, lane);
-      if (w + (int)gridDim.x < total) {
-        next = tile_of(w + gridDim.x, t.e);
+      if (tl + 1 < items) {
+        next = tile_of(tile_at(tl + 1), t.e);
         if (!GLU) f4_fetch_weights<F4_ROWS>(p, next.row0, next.rows, turn, lane, rw);
       }
       const int buf = tl & 1;
-      if (!ptx::mbar_wait_warp<true>(tfull_bar(buf), (tl >> 1) & 1, abort_flag, global_abort)) { timeout(1); break; }
+      if (!ptx::mbar_wait_warp<false, HINT>(tfull_bar(buf), (tl >> 1) & 1, abort_flag, global_abort)) { timeout(1); break; }
       ptx::tc_fence_after();
       const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * BUF_COLS);
+      const bool whole = !SHARE || (kb_begin(tl) == 0 && kb_end(tl) == KB);
+      bool mine = true;   // the sums are complete and this warp's to finish
+      if constexpr (SHARE) {
+        if (!whole && turn * 16 < t.rows) {
+          const int w = tile_at(tl), first = w * KB / per, last = ((w + 1) * KB - 1) / per;   // CTAs that share the tile
 #pragma unroll 1
-      for (int r0 = turn * 16; r0 < t.rows; r0 += 32) {   // the two warps of a quarter take turns
+          for (int r0 = turn * 16; r0 < t.rows; r0 += 32) {
+            uint32_t a[16], b[16];
+            ptx::tmem_ld16(taddr + r0, a);
+            ptx::tmem_ld16(taddr + F4_ROWS + r0, b);
+            ptx::tmem_ld_wait_on(a, b);
+            float* to = slot(2 * blockIdx.x + (kb_begin(tl) == 0 ? 1 : 0), r0);
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+              if (r0 + r < t.rows) {
+                __stcg(to + r * 256, __uint_as_float(a[r]));
+                __stcg(to + r * 256 + 128, __uint_as_float(b[r]));
+              }
+          }
+          __threadfence();
+          __syncwarp();
+          int before = 0;
+          if (lane == 0) before = atomicAdd(p.arrived + first * EPI_WARPS + warp, 1);
+          mine = __shfl_sync(0xFFFFFFFFu, before, 0) == last - first;
+          __threadfence();
+          for (int r0 = turn * 16; mine && r0 < t.rows; r0 += 32)
+#pragma unroll 1
+            for (int r = r0; r < min(r0 + 16, t.rows); ++r) {   // back into the accumulator, four parts on their way at once
+              float a = 0.f, b = 0.f;
+#pragma unroll 1
+              for (int i0 = first; i0 <= last; i0 += 4) {
+                float va[4], vb[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  const float* from = slot(2 * min(i0 + i, last) + (i0 + i == first ? 1 : 0), r);
+                  va[i] = i0 + i <= last ? __ldcg(from) : 0.f;
+                  vb[i] = i0 + i <= last ? __ldcg(from + 128) : 0.f;
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) { a += va[i]; b += vb[i]; }
+              }
+              ptx::tmem_st1(taddr + r, __float_as_uint(a));
+              ptx::tmem_st1(taddr + F4_ROWS + r, __float_as_uint(b));
+            }
+          ptx::tmem_st_wait();
+        }
+      }
+#pragma unroll 1
+      for (int r0 = turn * 16; mine && r0 < t.rows; r0 += 32) {   // the two warps of a quarter take turns
         uint32_t a[16], b[16];
         ptx::tmem_ld16(taddr + r0, a);
         ptx::tmem_ld16(taddr + F4_ROWS + r0, b);
@@ -183,14 +248,15 @@ ffn_fp4_kernel(const __grid_constant__ CUtensorMap map_wa, const __grid_constant
     if (lane == 0) {
       uint32_t it = 0;
       int e = 0;
-      for (int w = blockIdx.x; w < total && !*abort_flag; w += gridDim.x) {
-        const F4Tile t = tile_of(w, e);
+      for (int j = 0; j < items && !*abort_flag; ++j) {
+        const F4Tile t = tile_of(tile_at(j), e);
         e = t.e;
         const int box = (t.rows + 31) / 32;   // rows by 32; what the stage held behind them reaches no stored row
         const uint32_t bytes = (uint32_t)(t.halves * (W_BYTES + SF_BYTES) + box * 32 * 128 + SF_BYTES);
         const size_t wc0 = (size_t)t.e * p.NC + t.c0, wc1 = GLU ? wc0 : wc0 + 1;
         bool ok = true;
-        for (int kb = 0; kb < KB; ++kb, ++it) {
+        const int end = kb_end(j);
+        for (int kb = kb_begin(j); kb < end; ++kb, ++it) {
           const int s = it % NSTAGE;
           if (!ptx::mbar_wait<false, HINT>(empty_bar(s), ((it / NSTAGE) & 1) ^ 1, abort_flag, global_abort)) {
             timeout(2); ok = false; break;
@@ -218,16 +284,17 @@ ffn_fp4_kernel(const __grid_constant__ CUtensorMap map_wa, const __grid_constant
     int s = 0, tl = 0, e = 0;
     uint32_t ph = 0;
     bool ok = true;
-    for (int w = blockIdx.x; ok && w < total && !*abort_flag; w += gridDim.x, ++tl) {
+    for (; ok && tl < items && !*abort_flag; ++tl) {
       const int buf = tl & 1;
-      const F4Tile t = tile_of(w, e);
+      const F4Tile t = tile_of(tile_at(tl), e);
       e = t.e;
       if (!ptx::mbar_wait(tempty_bar(buf), ((tl >> 1) & 1) ^ 1, abort_flag, global_abort)) { timeout(3); break; }
       ptx::tc_fence_after();
       const uint32_t d = tmem + (uint32_t)(buf * BUF_COLS);
       const int n = (t.rows + 15) & ~15;
       const uint32_t id0 = idesc_f4(128, n, 0), id1 = idesc_f4(128, n, 2);
-      for (int kb = 0; kb < KB; ++kb) {
+      const int begin = kb_begin(tl), end = kb_end(tl);
+      for (int kb = begin; kb < end; ++kb) {
         if (!ptx::mbar_wait(full_bar(s), ph, abort_flag, global_abort)) { timeout(4); ok = false; break; }
         ptx::tc_fence_after();
         if (elected) {
@@ -239,9 +306,9 @@ ffn_fp4_kernel(const __grid_constant__ CUtensorMap map_wa, const __grid_constant
 #pragma unroll
           for (int k = 0; k < 4; ++k) {   // 64 of K: 32 bytes inside the swizzle row
             const uint32_t id = (k & 1) ? id1 : id0, ch = (uint32_t)(4 * (k >> 1));
-            ptx::umma_f4(d, w_desc + so + 2 * k, x_desc + so + 2 * k, id, sf + 8 + ch, sf + ch, (kb | k) != 0);
+            ptx::umma_f4(d, w_desc + so + 2 * k, x_desc + so + 2 * k, id, sf + 8 + ch, sf + ch, kb > begin || k > 0);
             if (t.halves > 1)
-              ptx::umma_f4(d + F4_ROWS, w_desc + so + (W_BYTES >> 4) + 2 * k, x_desc + so + 2 * k, id, sf + 16 + ch, sf + ch, (kb | k) != 0);
+              ptx::umma_f4(d + F4_ROWS, w_desc + so + (W_BYTES >> 4) + 2 * k, x_desc + so + 2 * k, id, sf + 16 + ch, sf + ch, kb > begin || k > 0);
           }
           ptx::umma_commit(empty_bar(s));   // free the stage when these UMMAs have read it
         }
@@ -269,7 +336,8 @@ __global__ void __launch_bounds__(256) fp4_sort_kernel(const uint4* __restrict__
                                                        const int32_t* __restrict__ gather_idx, int gather_div,
                                                        const int32_t* __restrict__ expert_offsets, int E, int K, int capacity, int tile_rows,
                                                        int chunk, uint4* xs, uint8_t* sfx, const float* __restrict__ topk_w,
-                                                       const int32_t* __restrict__ row_pair, float* row_w, int32_t* status) {
+                                                       const int32_t* __restrict__ row_pair, float* row_w, int32_t* arrived, int n_arrived,
+                                                       int32_t* status) {
   __shared__ int eoff[MAX_E + 1], tp[MAX_E + 1];
   grid_dependency_sync();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -277,6 +345,8 @@ __global__ void __launch_bounds__(256) fp4_sort_kernel(const uint4* __restrict__
   const long long r0 = ((long long)blockIdx.x * 8 + warp) * chunk;
   const int n = (int)max(0ll, min((long long)chunk, min((long long)__ldg(expert_offsets + E), (long long)capacity) - r0));   // rows of this warp
   f4_load_offsets(expert_offsets, E, eoff);
+  if (blockIdx.x == 0)
+    for (int i = threadIdx.x; i < n_arrived; i += 256) arrived[i] = 0;   // for the products behind this kernel
   int src = -1;
   if (lane < n) {
     const int r = (int)r0 + lane;
@@ -324,12 +394,12 @@ __global__ void __launch_bounds__(256) fp4_sort_kernel(const uint4* __restrict__
   }
 }
 
-template <bool GLU>
-cudaError_t launch_gemm(const F4Params& p, const void* wa, const void* wb, const void* rows, long long n_rows, cudaStream_t st) {
+template <bool GLU, bool SHARE>
+cudaError_t launch_form(const F4Params& p, const void* wa, const void* wb, const void* rows, long long n_rows, cudaStream_t st) {
   static std::atomic<bool> attr_set[MAX_DEVICES];   // per device; setting it twice is harmless
   const int dev = current_device();
   if (!attr_set[dev].load(std::memory_order_acquire)) {
-    const cudaError_t e = cudaFuncSetAttribute(ffn_fp4_kernel<GLU>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
+    const cudaError_t e = cudaFuncSetAttribute(ffn_fp4_kernel<GLU, SHARE>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
     if (e != cudaSuccess) return e;
     attr_set[dev].store(true, std::memory_order_release);
   }
@@ -339,7 +409,12 @@ cudaError_t launch_gemm(const F4Params& p, const void* wa, const void* wb, const
   for (int i = 0; i < 4; ++i)
     if (!make_act_map(&x.m[i], rows, n_rows, p.K / 2, true, 32 * (i + 1))) return cudaErrorInvalidValue;
   ProfileScope prof(GLU ? KID_GEMM1 : KID_GEMM2, st);
-  return launch_pdl(ffn_fp4_kernel<GLU>, dim3(sm_count()), dim3(THREADS), SMEM_BYTES, st, m_a, m_b, x, p);
+  return launch_pdl(ffn_fp4_kernel<GLU, SHARE>, dim3(min(sm_count(), F4_CTAS)), dim3(THREADS), SMEM_BYTES, st, m_a, m_b, x, p);
+}
+
+template <bool GLU>
+cudaError_t launch_gemm(const F4Params& p, const void* wa, const void* wb, const void* rows, long long n_rows, bool share, cudaStream_t st) {
+  return share ? launch_form<GLU, true>(p, wa, wb, rows, n_rows, st) : launch_form<GLU, false>(p, wa, wb, rows, n_rows, st);
 }
 
 }  // namespace
@@ -353,6 +428,24 @@ long long fp4_row_sets(const Shape& s) {
 
 static bool fp4_pairs(const Shape& s) { return (long long)s.T * s.k >= 256ll * s.E; }
 
+// Whether a product's tiles (at most row_tiles * ceil(N / width)) are shared.  A CTA streams at most 63 KB/us, all together 6.5 TB/s: tiles that leave SMs
+// idle take KB * 0.55 us whole, tiles * KB * 0.0052 us shared and then about 4 us for their parts.
+static bool fp4_share(const Shape& s, int K, int N, int width) {
+  const long long P = (long long)s.T * s.k, row_tiles = P / ffn::F4_ROWS + (s.E < P ? s.E : P);
+  const long long tiles = row_tiles * ((N + width - 1) / width), KB = (K + ffn::F4_BK - 1) / ffn::F4_BK;
+  return !fp4_pairs(s) && KB * (105 - tiles) > 770;
+}
+static bool fp4_share1(const Shape& s) { return fp4_share(s, s.d, s.f, 128); }
+static bool fp4_share2(const Shape& s) { return fp4_share(s, s.f, s.d, 256); }
+static int fp4_part_rows(const Shape& s) {
+  const long long P = (long long)s.T * s.k;
+  return P < ffn::F4_ROWS ? (int)(P + 15) & ~15 : ffn::F4_ROWS;
+}
+size_t fp4_part_bytes(const Shape& s) {
+  return fp4_share1(s) || fp4_share2(s) ? (size_t)2 * ffn::F4_CTAS * fp4_part_rows(s) * 256 * 4 : 0;
+}
+size_t fp4_arrived_bytes(const Shape& s) { return fp4_share1(s) || fp4_share2(s) ? (size_t)2 * ffn::F4_CTAS * 8 * 4 : 0; }
+
 cudaError_t launch_expert_ffn_fp4(const Shape& s, const FfnArgs& a, const Fp4Args& q, cudaStream_t st) {
   if (s.T == 0) return cudaSuccess;
   const int P = s.T * s.k;
@@ -362,7 +455,7 @@ cudaError_t launch_expert_ffn_fp4(const Shape& s, const FfnArgs& a, const Fp4Arg
   const int chunk = P >= 8 * 64 * sm_count() ? 8 : 1;   // rows per warp: one as long as all of them are resident at once
   cudaError_t e = launch_pdl(ffn::fp4_sort_kernel, dim3((unsigned)((P + 8 * chunk - 1) / (8 * chunk))), dim3(256), 0, st, static_cast<const uint4*>(a.a_src),
                              q.sx, a.a_rows, a.gather_idx, a.gather_div, a.expert_offsets, s.E, s.d, P, rows1, chunk, static_cast<uint4*>(a.xs), q.sfx,
-                             a.topk_w, a.row_pair, row_w, a.status);
+                             a.topk_w, a.row_pair, row_w, q.arrived, (int)(fp4_arrived_bytes(s) / 4), a.status);
   if (e != cudaSuccess) return e;
   ffn::F4Params g1{};
   g1.expert_offsets = a.expert_offsets;
@@ -376,8 +469,11 @@ cudaError_t launch_expert_ffn_fp4(const Shape& s, const FfnArgs& a, const Fp4Arg
   g1.hq = static_cast<uint32_t*>(a.h);
   g1.sfh = q.sfh;
   g1.h_rows = rows2;
+  g1.part = q.part;
+  g1.part_rows = fp4_part_rows(s);
+  g1.arrived = q.arrived;
   g1.status = a.status;
-  e = pairs ? ffn::launch_fp4_pair(true, g1, a.w1, a.w3, a.xs, P, fp4_row_sets(s), st) : ffn::launch_gemm<true>(g1, a.w1, a.w3, a.xs, P, st);
+  e = pairs ? ffn::launch_fp4_pair(true, g1, a.w1, a.w3, a.xs, P, fp4_row_sets(s), st) : ffn::launch_gemm<true>(g1, a.w1, a.w3, a.xs, P, fp4_share1(s), st);
   if (e != cudaSuccess) return e;
   ffn::F4Params g2{};
   g2.expert_offsets = a.expert_offsets;
@@ -389,8 +485,11 @@ cudaError_t launch_expert_ffn_fp4(const Shape& s, const FfnArgs& a, const Fp4Arg
   g2.sfa = g2.sfb = q.s2;
   g2.out = static_cast<__nv_bfloat16*>(a.o);
   g2.row_w = row_w;
+  g2.part = q.part;
+  g2.part_rows = g1.part_rows;
+  g2.arrived = q.arrived + ffn::F4_CTAS * 8;
   g2.status = a.status;
-  return pairs ? ffn::launch_fp4_pair(false, g2, a.w2, a.w2, a.h, P, fp4_row_sets(s), st) : ffn::launch_gemm<false>(g2, a.w2, a.w2, a.h, P, st);
+  return pairs ? ffn::launch_fp4_pair(false, g2, a.w2, a.w2, a.h, P, fp4_row_sets(s), st) : ffn::launch_gemm<false>(g2, a.w2, a.w2, a.h, P, fp4_share2(s), st);
 }
 
 }  // namespace tcmoe

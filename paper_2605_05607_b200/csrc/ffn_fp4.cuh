@@ -13,6 +13,8 @@ constexpr int F4_ROWS = 96;          // single CTA: two accumulators of 2 x 96 c
 constexpr int F4_PAIR_ROWS1 = 256;   // GEMM-1 on pairs: rows are the M side
 constexpr int F4_PAIR_ROWS2 = 192;   // GEMM-2 on pairs: two accumulators of 192 columns and the scales of five stages
 
+constexpr int F4_CTAS = 160;         // CTAs of the single-CTA products, at most (they have two slots for parts of tiles each)
+
 struct F4RowMaps { CUtensorMap m[4]; };   // boxes of 32, 64, 96, 128 rows
 
 struct F4Params {
@@ -26,6 +28,9 @@ struct F4Params {
   int h_rows;
   __nv_bfloat16* out;       // GEMM-2: o [P, N]
   const float* row_w;       // gate weight of every sorted row; NULL: 1
+  float* part;              // single CTAs: parts of tiles, two slots of part_rows rows x 256 columns per CTA
+  int part_rows;
+  int32_t* arrived;         // [F4_CTAS, 8 warps] parts of a tile that have been written, zero before the launch
   int32_t* status;
 };
 

@@ -7,6 +7,7 @@
 // The product with w comes first so that one pass has both sums of the row: rounding is monotone, so max|y| is (max|s * w|) * rstd to the bit.
 //
 // Bound by memory: every input is read once into registers and every output written once.
+#include "ptx.cuh"
 #include "quant.cuh"
 #include "quant4.cuh"
 
@@ -147,52 +148,66 @@ struct NormBwdArgs {
   float* part;            // [grid, columns]
 };
 
-template <int KEEP, int WARPS, bool SKIP>
+// Rows come through shared memory, STAGES of them on their way per block: every thread copies (cp.async) the vectors that it will use itself, so it waits
+// for its own copies and for nobody.  Loaded into registers instead, a row at a time, 8192 rows of 4096 with dres took 67 us, XXX so.
+template <int KEEP, int WARPS, int STAGES, bool SKIP>
 __global__ void __launch_bounds__(WARPS * 32) rmsnorm_backward_kernel(const NormBwdArgs a) {
-  grid_dependency_sync();
-  constexpr int LANES = WARPS * 32;
+  extern __shared__ __align__(16) uint4 ring[];   // [STAGES][dy, s, dres][vec_per_row]
+  constexpr int LANES = WARPS * 32, STREAMS = SKIP ? 3 : 2;
   __shared__ float part[2][WARPS];
-  const int lane = threadIdx.x;
-  float dw[KEEP][VEC];
+  grid_dependency_sync();
+  const int lane = threadIdx.x, n_vec = a.vec_per_row;
+  const uint4* const from[3] = {a.dy, a.s, a.dres};
+  auto fetch = [&](int r, int stage) {
+    if (r < a.rows) {
 #pragma unroll
-  for (int i = 0; i < KEEP; ++i)
+      for (int q = 0; q < STREAMS; ++q)
+#pragma unroll
+        for (int i = 0; i < KEEP; ++i) {
+          const int v = lane + LANES * i;
+          if (v < n_vec) ptx::cp_async_16(ptx::smem_u32(ring + (stage * STREAMS + q) * n_vec + v), from[q] + (long long)r * n_vec + v, 16);
+        }
+    }
+    ptx::cp_async_commit();
+  };
+#pragma unroll
+  for (int i = 0; i < STAGES; ++i) fetch(blockIdx.x + i * gridDim.x, i);
+  float dw[KEEP][VEC], w[KEEP][VEC];
+#pragma unroll
+  for (int i = 0; i < KEEP; ++i) {
 #pragma unroll
     for (int j = 0; j < VEC; ++j) dw[i][j] = 0.f;
-  int flip = 0;
-  const float n = (float)(a.vec_per_row * VEC);
+    if (lane + LANES * i < n_vec) load_w(a.w, a.w32, lane + LANES * i, w[i]);
+  }
+  int flip = 0, stage = 0;
+  const float n = (float)(n_vec * VEC);
+  float rstd = blockIdx.x < a.rows ? __ldg(a.rstd + blockIdx.x) : 0.f;
   for (int r = blockIdx.x; r < a.rows; r += gridDim.x) {
-    const long long base = (long long)r * a.vec_per_row;
+    const float next = r + (int)gridDim.x < a.rows ? __ldg(a.rstd + r + gridDim.x) : 0.f;
+    ptx::cp_async_wait<STAGES - 1>();   // this row's copies of this thread
     uint4 dyv[KEEP], sv[KEEP], kv[SKIP ? KEEP : 1];
-#pragma unroll
-    for (int i = 0; i < KEEP; ++i) {
-      const int v = lane + LANES * i;
-      if (v < a.vec_per_row) {
-        dyv[i] = a.dy[base + v];
-        sv[i] = a.s[base + v];
-        if (SKIP) kv[i] = a.dres[base + v];
-      }
-    }
-    const float rstd = __ldg(a.rstd + r);
     float dot = 0.f;
 #pragma unroll
     for (int i = 0; i < KEEP; ++i) {
       const int v = lane + LANES * i;
-      if (v < a.vec_per_row) {
-        float dy[VEC], s[VEC], w[VEC];
+      if (v < n_vec) {
+        dyv[i] = ring[(stage * STREAMS) * n_vec + v];
+        sv[i] = ring[(stage * STREAMS + 1) * n_vec + v];
+        if (SKIP) kv[i] = ring[(stage * STREAMS + 2) * n_vec + v];
+        float dy[VEC], s[VEC];
         unpack8(dyv[i], dy);
         unpack8(sv[i], s);
-        load_w(a.w, a.w32, v, w);
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
           const float t = dy[j] * (s[j] * rstd);
           dw[i][j] += t;
-          dot = fmaf(t, w[j], dot);
+          dot = fmaf(t, w[i][j], dot);
         }
       }
     }
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, off);
-    if (WARPS > 1) {
+    if (WARPS > 1) {   // two buffers: the next row's sums do not overwrite what a slow warp still reads
       if ((lane & 31) == 0) part[flip][lane >> 5] = dot;
       __syncthreads();
       dot = 0.f;
@@ -200,53 +215,55 @@ __global__ void __launch_bounds__(WARPS * 32) rmsnorm_backward_kernel(const Norm
       for (int i = 0; i < WARPS; ++i) dot += part[flip][i];
       flip ^= 1;
     }
+    fetch(r + STAGES * gridDim.x, stage);   // the stage's values are in registers (their sum has been used)
+    if (++stage == STAGES) stage = 0;
     const float mean = dot / n;
 #pragma unroll
     for (int i = 0; i < KEEP; ++i) {
       const int v = lane + LANES * i;
-      if (v < a.vec_per_row) {
-        float dy[VEC], s[VEC], w[VEC], k[VEC];
+      if (v < n_vec) {
+        float dy[VEC], s[VEC], k[VEC];
         unpack8(dyv[i], dy);
         unpack8(sv[i], s);
-        load_w(a.w, a.w32, v, w);
         if (SKIP) unpack8(kv[i], k);
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
-          const float g = (dy[j] * w[j] - (s[j] * rstd) * mean) * rstd;
+          const float g = (dy[j] * w[i][j] - (s[j] * rstd) * mean) * rstd;
           s[j] = SKIP ? g + k[j] : g;
         }
-        a.dx[base + v] = pack8(s);
+        a.dx[(long long)r * n_vec + v] = pack8(s);
       }
     }
+    rstd = next;
   }
 #pragma unroll
   for (int i = 0; i < KEEP; ++i) {
     const int v = lane + LANES * i;
-    if (v < a.vec_per_row) {
-      float4* out = reinterpret_cast<float4*>(a.part + (long long)blockIdx.x * a.vec_per_row * VEC) + 2 * v;
+    if (v < n_vec) {
+      float4* out = reinterpret_cast<float4*>(a.part + (long long)blockIdx.x * n_vec * VEC) + 2 * v;
       out[0] = make_float4(dw[i][0], dw[i][1], dw[i][2], dw[i][3]);
       out[1] = make_float4(dw[i][4], dw[i][5], dw[i][6], dw[i][7]);
     }
   }
 }
 
-// dw[c] = sum over the blocks' partial rows: 32 columns per block, eight warps share the rows.
-__global__ void __launch_bounds__(256) rmsnorm_dw_kernel(const float* __restrict__ part, int parts, int cols, float* __restrict__ dw) {
+// dw[c] = sum over the blocks' partial rows: 32 columns per block, whose warps share the rows (a load of each is on its way at once: eight
+// warps instead of 32 took 10 us for 592 partial rows of 4096).
+__global__ void __launch_bounds__(1024) rmsnorm_dw_kernel(const float* __restrict__ part, int parts, int cols, float* __restrict__ dw) {
   grid_dependency_sync();
-  __shared__ float sum_s[8][32];
+  __shared__ float sum_s[32][33];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
   float sum = 0.f;
   if (c < cols) {
-#pragma unroll 4
-    for (int r = warp; r < parts; r += 8) sum += part[(long long)r * cols + c];
+#pragma unroll 10
+    for (int r = warp; r < parts; r += 32) sum += part[(long long)r * cols + c];
   }
   sum_s[warp][lane] = sum;
   __syncthreads();
-  if (warp == 0 && c < cols) {
+  sum = sum_s[lane][warp];
 #pragma unroll
-    for (int i = 1; i < 8; ++i) sum += sum_s[i][lane];
-    dw[c] = sum;
-  }
+  for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, off);
+  if (lane == 0 && blockIdx.x * 32 + warp < cols) dw[blockIdx.x * 32 + warp] = sum;
 }
 
 template <bool RES, bool QUANT>
@@ -265,16 +282,26 @@ cudaError_t launch_norm(const NormArgs& a, cudaStream_t st) {
   return go(rmsnorm_kernel<4, 16, RES, QUANT>, 512, 1);   // NORM_COLS
 }
 
+// Blocks per SM as shared memory, registers and NORM_PARTS (four per SM) allow.
 template <bool SKIP>
-cudaError_t launch_norm_bwd(const NormBwdArgs& a, int grid, cudaStream_t st) {
+cudaError_t launch_norm_bwd(const NormBwdArgs& a, int* parts, cudaStream_t st) {
   const int cols = a.vec_per_row * VEC;
-  auto go = [&](auto kernel, int threads) { return launch_pdl(kernel, dim3(grid), dim3(threads), 0, st, a); };
-  if (cols <= 512) return go(rmsnorm_backward_kernel<1, 2, SKIP>, 64);
-  if (cols <= 1024) return go(rmsnorm_backward_kernel<1, 4, SKIP>, 128);
-  if (cols <= 2048) return go(rmsnorm_backward_kernel<1, 8, SKIP>, 256);
-  if (cols <= 4096) return go(rmsnorm_backward_kernel<2, 8, SKIP>, 256);
-  if (cols <= 8192) return go(rmsnorm_backward_kernel<2, 16, SKIP>, 512);
-  return go(rmsnorm_backward_kernel<4, 16, SKIP>, 512);   // NORM_COLS
+  auto go = [&](auto kernel, int threads, int stages) {
+    const int smem = stages * (SKIP ? 3 : 2) * cols * 2;
+    if (smem > 40 * 1024) {   // beyond 48 KiB with what the kernel declares itself
+      const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+      if (e != cudaSuccess) return e;
+    }
+    const int per_sm = max(1, min(min(4, 1024 / threads), 226 * 1024 / (smem + 1280)));
+    *parts = min(min(a.rows, NORM_PARTS), per_sm * sm_count());
+    return launch_pdl(kernel, dim3(*parts), dim3(threads), smem, st, a);
+  };
+  if (cols <= 512) return go(rmsnorm_backward_kernel<1, 2, 4, SKIP>, 64, 4);
+  if (cols <= 1024) return go(rmsnorm_backward_kernel<1, 4, 4, SKIP>, 128, 4);
+  if (cols <= 2048) return go(rmsnorm_backward_kernel<1, 8, 4, SKIP>, 256, 4);
+  if (cols <= 4096) return go(rmsnorm_backward_kernel<2, 8, 3, SKIP>, 256, 3);
+  if (cols <= 8192) return go(rmsnorm_backward_kernel<2, 16, 3, SKIP>, 512, 3);
+  return go(rmsnorm_backward_kernel<4, 16, 2, SKIP>, 512, 2);   // NORM_COLS
 }
 
 }  // namespace
@@ -292,14 +319,14 @@ int rmsnorm_parts(long long rows) { return (int)(rows < NORM_PARTS ? rows : NORM
 
 cudaError_t launch_rmsnorm_backward(const void* dy, const void* dres, const void* s, const void* w, bool w32, const float* rstd,
                                     long long rows, int cols, void* dx, float* dw, float* part, cudaStream_t st) {
-  const int parts = rmsnorm_parts(rows);
-  if (parts > 0) {
+  int parts = 0;
+  if (rows > 0) {
     const NormBwdArgs a{static_cast<const uint4*>(dy), static_cast<const uint4*>(dres), static_cast<const uint4*>(s), w, w32 ? 1 : 0, rstd,
                         (int)rows, cols / VEC, static_cast<uint4*>(dx), part};
-    const cudaError_t e = dres != nullptr ? launch_norm_bwd<true>(a, parts, st) : launch_norm_bwd<false>(a, parts, st);
+    const cudaError_t e = dres != nullptr ? launch_norm_bwd<true>(a, &parts, st) : launch_norm_bwd<false>(a, &parts, st);
     if (e != cudaSuccess) return e;
   }
-  return launch_pdl(rmsnorm_dw_kernel, dim3((cols + 31) / 32), dim3(256), 0, st, static_cast<const float*>(part), parts, cols, dw);
+  return launch_pdl(rmsnorm_dw_kernel, dim3((cols + 31) / 32), dim3(1024), 0, st, static_cast<const float*>(part), parts, cols, dw);
 }
 
 }  // namespace tcmoe
