@@ -149,14 +149,17 @@ struct NormBwdArgs {
 };
 
 // Rows come through shared memory, STAGES of them on their way per block: every thread copies (cp.async) the vectors that it will use itself, so it waits
-// for its own copies and for nobody.  Loaded into registers instead, a row at a time, 8192 rows of 4096 with dres took 67 us, XXX so.
+// for its own copies and for nobody.  Loaded into registers instead, a row at a time, 8192 rows of 4096 with dres took 67 us, 49 so.
+// WARPS warps per row; WARPS == 1: eight rows per block, whose dw are joined at the end (16000 rows of 512 with two warps per row: 35.9 us, 18.6 so).
 template <int KEEP, int WARPS, int STAGES, bool SKIP>
-__global__ void __launch_bounds__(WARPS * 32) rmsnorm_backward_kernel(const NormBwdArgs a) {
-  extern __shared__ __align__(16) uint4 ring[];   // [STAGES][dy, s, dres][vec_per_row]
-  constexpr int LANES = WARPS * 32, STREAMS = SKIP ? 3 : 2;
+__global__ void __launch_bounds__(WARPS == 1 ? 256 : WARPS * 32) rmsnorm_backward_kernel(const NormBwdArgs a) {
+  extern __shared__ __align__(16) uint4 ring_s[];   // per row of the block: [STAGES][dy, s, dres][vec_per_row]
+  constexpr int LANES = WARPS * 32, STREAMS = SKIP ? 3 : 2, TEAMS = WARPS == 1 ? 8 : 1;
   __shared__ float part[2][WARPS];
   grid_dependency_sync();
-  const int lane = threadIdx.x, n_vec = a.vec_per_row;
+  const int lane = WARPS == 1 ? threadIdx.x & 31 : threadIdx.x, team = WARPS == 1 ? threadIdx.x >> 5 : 0, n_vec = a.vec_per_row;
+  const int r0 = blockIdx.x * TEAMS + team, step = gridDim.x * TEAMS;
+  uint4* ring = ring_s + team * STAGES * STREAMS * n_vec;
   const uint4* const from[3] = {a.dy, a.s, a.dres};
   auto fetch = [&](int r, int stage) {
     if (r < a.rows) {
@@ -171,7 +174,7 @@ __global__ void __launch_bounds__(WARPS * 32) rmsnorm_backward_kernel(const Norm
     ptx::cp_async_commit();
   };
 #pragma unroll
-  for (int i = 0; i < STAGES; ++i) fetch(blockIdx.x + i * gridDim.x, i);
+  for (int i = 0; i < STAGES; ++i) fetch(r0 + i * step, i);
   float dw[KEEP][VEC], w[KEEP][VEC];
 #pragma unroll
   for (int i = 0; i < KEEP; ++i) {
@@ -181,9 +184,9 @@ __global__ void __launch_bounds__(WARPS * 32) rmsnorm_backward_kernel(const Norm
   }
   int flip = 0, stage = 0;
   const float n = (float)(n_vec * VEC);
-  float rstd = blockIdx.x < a.rows ? __ldg(a.rstd + blockIdx.x) : 0.f;
-  for (int r = blockIdx.x; r < a.rows; r += gridDim.x) {
-    const float next = r + (int)gridDim.x < a.rows ? __ldg(a.rstd + r + gridDim.x) : 0.f;
+  float rstd = r0 < a.rows ? __ldg(a.rstd + r0) : 0.f;
+  for (int r = r0; r < a.rows; r += step) {
+    const float next = r + step < a.rows ? __ldg(a.rstd + r + step) : 0.f;
     ptx::cp_async_wait<STAGES - 1>();   // this row's copies of this thread
     uint4 dyv[KEEP], sv[KEEP], kv[SKIP ? KEEP : 1];
     float dot = 0.f;
@@ -215,7 +218,7 @@ __global__ void __launch_bounds__(WARPS * 32) rmsnorm_backward_kernel(const Norm
       for (int i = 0; i < WARPS; ++i) dot += part[flip][i];
       flip ^= 1;
     }
-    fetch(r + STAGES * gridDim.x, stage);   // the stage's values are in registers (their sum has been used)
+    fetch(r + STAGES * step, stage);   // the stage's values are in registers (their sum has been used)
     if (++stage == STAGES) stage = 0;
     const float mean = dot / n;
 #pragma unroll
@@ -235,6 +238,26 @@ __global__ void __launch_bounds__(WARPS * 32) rmsnorm_backward_kernel(const Norm
       }
     }
     rstd = next;
+  }
+  if (WARPS == 1) {   // the block's eight sums, a column at a time, in the order of the warps
+    ptx::cp_async_wait<0>();
+    __syncthreads();
+    float* sums = reinterpret_cast<float*>(ring_s);   // [8][columns]: fits, as a warp's ring has STAGES * STREAMS * 2 >= 4 bytes per column
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i) {
+      const int v = lane + LANES * i;
+      if (v < n_vec)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) sums[(team * n_vec + v) * VEC + j] = dw[i][j];
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < n_vec * VEC; c += 256) {
+      float sum = 0.f;
+#pragma unroll
+      for (int t = 0; t < TEAMS; ++t) sum += sums[t * n_vec * VEC + c];
+      a.part[(long long)blockIdx.x * n_vec * VEC + c] = sum;
+    }
+    return;
   }
 #pragma unroll
   for (int i = 0; i < KEEP; ++i) {
@@ -286,20 +309,20 @@ cudaError_t launch_norm(const NormArgs& a, cudaStream_t st) {
 template <bool SKIP>
 cudaError_t launch_norm_bwd(const NormBwdArgs& a, int* parts, cudaStream_t st) {
   const int cols = a.vec_per_row * VEC;
-  auto go = [&](auto kernel, int threads, int stages) {
-    const int smem = stages * (SKIP ? 3 : 2) * cols * 2;
+  auto go = [&](auto kernel, int threads, int stages, int teams = 1) {
+    const int smem = teams * stages * (SKIP ? 3 : 2) * cols * 2;
     if (smem > 40 * 1024) {   // beyond 48 KiB with what the kernel declares itself
       const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
       if (e != cudaSuccess) return e;
     }
     const int per_sm = max(1, min(min(4, 1024 / threads), 226 * 1024 / (smem + 1280)));
-    *parts = min(min(a.rows, NORM_PARTS), per_sm * sm_count());
+    *parts = min(min((a.rows + teams - 1) / teams, NORM_PARTS), per_sm * sm_count());
     return launch_pdl(kernel, dim3(*parts), dim3(threads), smem, st, a);
   };
-  if (cols <= 512) return go(rmsnorm_backward_kernel<1, 2, 4, SKIP>, 64, 4);
-  if (cols <= 1024) return go(rmsnorm_backward_kernel<1, 4, 4, SKIP>, 128, 4);
+  if (cols <= 512) return go(rmsnorm_backward_kernel<2, 1, 4, SKIP>, 256, 4, 8);
+  if (cols <= 1024) return go(rmsnorm_backward_kernel<4, 1, 3, SKIP>, 256, 3, 8);
   if (cols <= 2048) return go(rmsnorm_backward_kernel<1, 8, 4, SKIP>, 256, 4);
-  if (cols <= 4096) return go(rmsnorm_backward_kernel<2, 8, 3, SKIP>, 256, 3);
+  if (cols <= 4096) return go(rmsnorm_backward_kernel<1, 16, 4, SKIP>, 512, 4);
   if (cols <= 8192) return go(rmsnorm_backward_kernel<2, 16, 3, SKIP>, 512, 3);
   return go(rmsnorm_backward_kernel<4, 16, 2, SKIP>, 512, 2);   // NORM_COLS
 }
