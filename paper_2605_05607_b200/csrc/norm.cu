@@ -6,7 +6,8 @@
 // Everything is computed from the fp32 sum: y and the codes are rounded once each, from fp32 (codes of the rounded y would round twice).
 // The product with w comes first so that one pass has both sums of the row: rounding is monotone, so max|y| is (max|s * w|) * rstd to the bit.
 //
-// Bound by memory: every input is read once into registers and every output written once.
+// Bound by memory: every input is read once into registers and every output written once.  16384 rows of 4096 with residual, bf16 and E4M3 outputs
+// 106 us (5.7 TB/s); rows on their way through shared memory instead (as in the backward pass below) took 117.
 #include "ptx.cuh"
 #include "quant.cuh"
 #include "quant4.cuh"
@@ -291,18 +292,22 @@ __global__ void __launch_bounds__(1024) rmsnorm_dw_kernel(const float* __restric
 
 template <bool RES, bool QUANT>
 cudaError_t launch_norm(const NormArgs& a, cudaStream_t st) {
-  const long long cap = (long long)sm_count() * 16;
+  const int cols = a.vec_per_row * VEC;
+  // Blocks per SM before they take a second row, us with 16 / 64: 32768 rows of 2000, bf16 alone, 52.2 / 49.6, 16357 of 4096 51.3 / 47.7; with residual and
+  // both outputs 102.5 / 101.7; 9347 of 7168 110.9 / 113.1, 32768 of 512 28.6 / 29.4.
+  const long long cap = (long long)sm_count() * (cols > 1024 && cols <= 4096 ? 64 : 16);
   auto go = [&](auto kernel, int threads, int rpb) {
     const long long blocks = (a.rows + rpb - 1) / rpb;
     return launch_pdl(kernel, dim3((unsigned)(blocks < cap ? blocks : cap)), dim3(threads), 0, st, a);
   };
-  const int cols = a.vec_per_row * VEC;
   if (cols <= 512) return go(rmsnorm_kernel<2, 1, RES, QUANT>, 256, 8);
   if (cols <= 1024) return go(rmsnorm_kernel<4, 1, RES, QUANT>, 256, 8);
   if (cols <= 2048) return go(rmsnorm_kernel<2, 4, RES, QUANT>, 128, 1);
   if (cols <= 4096) return go(rmsnorm_kernel<4, 4, RES, QUANT>, 128, 1);
   if (cols <= 8192) return go(rmsnorm_kernel<4, 8, RES, QUANT>, 256, 1);
-  return go(rmsnorm_kernel<4, 16, RES, QUANT>, 512, 1);   // NORM_COLS
+  // to NORM_COLS; us with 256 / 512 threads per row: 4187 rows of 16000, bf16 alone, 53.5 / 79.4, with residual and both outputs (spilled) 160 / 115
+  if (RES) return go(rmsnorm_kernel<4, 16, RES, QUANT>, 512, 1);
+  return go(rmsnorm_kernel<8, 8, RES, QUANT>, 256, 1);
 }
 
 // Blocks per SM as shared memory, registers and NORM_PARTS (four per SM) allow.
