@@ -42,7 +42,7 @@ constexpr int NUM_BARS = 2 * NSTAGE + 4;
 constexpr int EPI_WARPS = 8, TMA_WARP = EPI_WARPS, MMA_WARP = EPI_WARPS + 1;
 constexpr int THREADS = (EPI_WARPS + 2) * 32;
 constexpr int TABLE_BYTES = (2 * (MAX_E + 1) * 4 + 15) & ~15;
-constexpr int SMEM_BYTES = 1024 + NSTAGE * STAGE_BYTES + NUM_BARS * 8 + 64 + TABLE_BYTES + EPI_WARPS * F4Out<F4_ROWS>::BYTES;
+constexpr int SMEM_BYTES = 1024 + NSTAGE * STAGE_BYTES + NUM_BARS * 8 + 64 + TABLE_BYTES + EPI_WARPS * F4Out<F4_ROWS, 2>::BYTES;
 static_assert(SMEM_BYTES <= 232448, "shared memory of an SM");
 constexpr uint32_t HINT = 1000;
 
@@ -131,24 +131,24 @@ ffn_fp4_kernel(const __grid_constant__ CUtensorMap map_wa, const __grid_constant
   if (warp < EPI_WARPS) {
     // ================================ epilogue: lane = column, TMEM column = row ================================
     const int quarter = warp & 3, turn = warp >> 2;
-    const uint32_t out_mem = ptx::smem_u32(tp_s) + TABLE_BYTES + (uint32_t)(warp * F4Out<F4_ROWS>::BYTES);   // GEMM-2
+    const uint32_t out_mem = ptx::smem_u32(tp_s) + TABLE_BYTES + (uint32_t)(warp * F4Out<F4_ROWS, 2>::BYTES);   // GEMM-2
     int tl = 0;
     F4Tile t{}, next{};
-    float rw[(F4Out<F4_ROWS>::TURNS + 1) / 2];
+    float rw[(F4Out<F4_ROWS, 2>::TURNS + 1) / 2];
     // slot 2 i: the part of CTA i's first tile, which began before it; slot 2 i + 1: that of its last, which goes on behind it
     auto slot = [&](int i, int r0) {
       return p.part + ((size_t)i * p.part_rows + r0) * 256 + quarter * 32 + lane;   // per row: 128 columns of either half
     };
     if (items > 0) {
       next = tile_of(tile_at(0), 0);
-      if (!GLU) f4_fetch_weights<F4_ROWS>(p, next.row0, next.rows, turn, lane, rw);
+      if (!GLU) f4_fetch_weights<F4_ROWS, 2>(p, next.row0, next.rows, turn, lane, rw);
     }
     for (; tl < items && !*abort_flag; ++tl) {
       t = next;
-      if (!GLU) f4_keep_weights<F4_ROWS>(rw, out_mem, lane);
+      if (!GLU) f4_keep_weights<F4_ROWS, 2>(rw, out_mem, lane);
       if (tl + 1 < items) {
         next = tile_of(tile_at(tl + 1), t.e);
-        if (!GLU) f4_fetch_weights<F4_ROWS>(p, next.row0, next.rows, turn, lane, rw);
+        if (!GLU) f4_fetch_weights<F4_ROWS, 2>(p, next.row0, next.rows, turn, lane, rw);
       }
       const int buf = tl & 1;
       if (!ptx::mbar_wait_warp<false, HINT>(tfull_bar(buf), (tl >> 1) & 1, abort_flag, global_abort)) { timeout(1); break; }
@@ -235,8 +235,8 @@ ffn_fp4_kernel(const __grid_constant__ CUtensorMap map_wa, const __grid_constant
           }
         } else {
           const int col0 = t.c0 * 128 + quarter * 32;
-          f4_store_rows<F4_ROWS>(p, a, out_mem, r0 >> 5, lane, t.row0 + r0, t.rows - r0, col0);
-          if (t.halves > 1) f4_store_rows<F4_ROWS>(p, b, out_mem, r0 >> 5, lane, t.row0 + r0, t.rows - r0, col0 + 128);
+          f4_store_rows<F4_ROWS, 2>(p, a, out_mem, r0 >> 5, lane, t.row0 + r0, t.rows - r0, col0);
+          if (t.halves > 1) f4_store_rows<F4_ROWS, 2>(p, b, out_mem, r0 >> 5, lane, t.row0 + r0, t.rows - r0, col0 + 128);
         }
       }
       ptx::tc_fence_before();
@@ -426,7 +426,12 @@ long long fp4_row_sets(const Shape& s) {
   return one > two ? one : two;
 }
 
-static bool fp4_pairs(const Shape& s) { return (long long)s.T * s.k >= 256ll * s.E; }
+// CTA pairs from 112 rows per expert on.  FFN on single CTAs / pairs, us, rows per expert in brackets: 3200 tokens, top-4 of 128 x 2048 x 1024 (100)
+// 161 / 139, 1777 skewed, top-4 of 64 x 2880 x 2880 (111) 246 / 270, 450, top-2 of 8 x 4096 x 4096 (112) 72 / 69, 1000 skewed, top-4 of
+// 32 x 1024 x 1024 (125) 52 / 41, 4096, top-2 of 64 x 2048 x 2048 (128) 174 / 134, 800, top-2 of 8 x 2048 x 7168 (200) 99 / 72, 3600 skewed on
+// 16 x 4096 x 1536 (225) 87 / 81.  (Both forms side by side, each for the experts of its kind, gained nothing where routing is skewed,
+// 246 / 243, and lost where tiles are few: 400 skewed, top-2 of 8 x 4096 x 4096, 69 / 85.)
+static bool fp4_pairs(const Shape& s) { return (long long)s.T * s.k >= 112ll * s.E; }
 
 // Whether a product's tiles (at most row_tiles * ceil(N / width)) are shared.  A CTA streams at most 63 KB/us, all together 6.5 TB/s: tiles that leave SMs
 // idle take KB * 0.55 us whole, tiles * KB * 0.0052 us shared and then about 4 us for their parts.

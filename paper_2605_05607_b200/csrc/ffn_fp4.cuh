@@ -11,11 +11,11 @@ constexpr int F4_SF_BYTES = 1024;                   // scales of 128 rows over a
 // Rows of a tile.  The scales of a row tile lie together, in one or two sets of chunks of 128 rows: whoever writes them needs the tile of the product that reads them.
 constexpr int F4_ROWS = 96;          // single CTA: two accumulators of 2 x 96 columns and the scales of four stages fit TMEM
 constexpr int F4_PAIR_ROWS1 = 256;   // GEMM-1 on pairs: rows are the M side
-constexpr int F4_PAIR_ROWS2 = 192;   // GEMM-2 on pairs: two accumulators of 192 columns and the scales of five stages
+constexpr int F4_PAIR_ROWS2 = 208;   // GEMM-2 on pairs: two accumulators of 208 columns and the scales of four stages
 
 constexpr int F4_CTAS = 160;         // CTAs of the single-CTA products, at most (they have two slots for parts of tiles each)
 
-struct F4RowMaps { CUtensorMap m[4]; };   // boxes of 32, 64, 96, 128 rows
+struct F4RowMaps { CUtensorMap m[4]; };   // boxes of 32, 64, 96 rows, and of as many as a CTA's half of a pair tile
 
 struct F4Params {
   const int32_t* expert_offsets;
@@ -55,6 +55,21 @@ __device__ __forceinline__ uint64_t scale_desc(uint32_t smem_addr) {
 __device__ __forceinline__ void f4_load_offsets(const int32_t* expert_offsets, int E, int* eoff) {
   for (int i = threadIdx.x; i <= E; i += blockDim.x) eoff[i] = __ldcg(expert_offsets + i);
 }
+// silu(a) * b = a b / (1 + 2^(-a log2 e)) of two values: products and sums two at a time (f32x2)
+__device__ __forceinline__ float2 silu_mul2(float a0, float a1, float b0, float b1) {
+  float2 h;
+  asm("{\n\t.reg .b64 a, b, t, c;\n\t.reg .f32 x, y;\n\t"
+      "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+      "mov.b64 c, {%6, %6};\n\tmul.rn.f32x2 t, a, c;\n\t"
+      "mov.b64 {x, y}, t;\n\tex2.approx.ftz.f32 x, x;\n\tex2.approx.ftz.f32 y, y;\n\tmov.b64 t, {x, y};\n\t"
+      "mov.b64 c, {%7, %7};\n\tadd.rn.f32x2 t, t, c;\n\t"
+      "mov.b64 {x, y}, t;\n\trcp.approx.ftz.f32 x, x;\n\trcp.approx.ftz.f32 y, y;\n\tmov.b64 t, {x, y};\n\t"
+      "mul.rn.f32x2 a, a, b;\n\tmul.rn.f32x2 t, a, t;\n\tmov.b64 {%0, %1}, t;\n\t}"
+      : "=f"(h.x), "=f"(h.y)
+      : "f"(a0), "f"(a1), "f"(b0), "f"(b1), "f"(-1.4426950408889634f), "f"(1.f));
+  return h;
+}
+
 // Tiles of `rows` rows per expert, exclusive prefix (tp[E] = all of them), by one warp.
 __device__ __forceinline__ void f4_tile_table(const int* eoff, int E, int rows, int* tp, int lane) {
   int base = 0;
@@ -80,7 +95,7 @@ __device__ __forceinline__ int f4_expert_from(const int* tp, int e, int n_tiles,
   return e;
 }
 
-// GEMM-2's epilogue: lane = column, TMEM column = row.  Two warps share a quarter of the columns and take turns of 16 rows; each has its own piece of
+// GEMM-2's epilogue: lane = column, TMEM column = row.  Two or four warps share a quarter of the columns and take turns of 16 rows; each has its own piece of
 // shared memory: the gate weights of its rows, then a buffer of 16 rows x 32 columns, two rows to a word.
 //
 // The weights are in the order of the rows (written by the kernel that sorts them) and are fetched a tile ahead: two dependent loads per 16 rows in the
@@ -88,31 +103,31 @@ __device__ __forceinline__ int f4_expert_from(const int* tp, int e, int n_tiles,
 // rows leave it in few instructions: 4 loads of weights, 8 stores of two rows' bf16 pair and 2 loads of eight columns per 16 x 32 values, and
 // 16-byte stores to o.
 constexpr int F4_OUT_PITCH = 36;   // words per two rows: lanes that load neighbouring rows use different banks
-template <int ROWS> struct F4Out {
-  static constexpr int TURNS = (ROWS + 31) / 32;
+template <int ROWS, int SHARES> struct F4Out {   // SHARES warps share a quarter
+  static constexpr int TURNS = (ROWS + 16 * SHARES - 1) / (16 * SHARES);
   static constexpr int BYTES = TURNS * 64 + 8 * F4_OUT_PITCH * 4;
 };
-// Lane l of w[i] has row 16 turn + 32 (j / 16) + j % 16, j = 32 i + l.
-template <int ROWS, int N>
-__device__ __forceinline__ void f4_fetch_weights(const F4Params& p, int row0, int rows, int turn, int lane, float (&w)[N]) {
-  static_assert(ROWS % 32 == 0 && N == (F4Out<ROWS>::TURNS + 1) / 2, "32 lanes: 16 rows of two turns");
+// Lane l of w[i] has row 16 (share + SHARES (j / 16)) + j % 16, j = 32 i + l.
+template <int ROWS, int SHARES, int N>
+__device__ __forceinline__ void f4_fetch_weights(const F4Params& p, int row0, int rows, int share, int lane, float (&w)[N]) {
+  static_assert(N == (F4Out<ROWS, SHARES>::TURNS + 1) / 2, "32 lanes: 16 rows of two turns");
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const int at = 32 * i + lane, r = 16 * turn + 32 * (at >> 4) + (at & 15);
+    const int at = 32 * i + lane, r = 16 * (share + SHARES * (at >> 4)) + (at & 15);
     w[i] = p.row_w != nullptr && r < rows ? __ldcg(p.row_w + row0 + r) : 1.f;
   }
 }
-template <int ROWS, int N>
+template <int ROWS, int SHARES, int N>
 __device__ __forceinline__ void f4_keep_weights(const float (&w)[N], uint32_t mem, int lane) {
 #pragma unroll
   for (int i = 0; i < N; ++i)
-    if (32 * i + lane < 16 * F4Out<ROWS>::TURNS) ptx::st_shared_b32(mem + 4 * (32 * i + lane), __float_as_uint(w[i]));
+    if (32 * i + lane < 16 * F4Out<ROWS, SHARES>::TURNS) ptx::st_shared_b32(mem + 4 * (32 * i + lane), __float_as_uint(w[i]));
   __syncwarp();
 }
 // turn `i` of the warp: 16 rows from row0 on, of which `rows` exist
-template <int ROWS>
+template <int ROWS, int SHARES>
 __device__ __forceinline__ void f4_store_rows(const F4Params& p, const uint32_t (&acc)[16], uint32_t mem, int i, int lane, int row0, int rows, int col0) {
-  const uint32_t buf = mem + F4Out<ROWS>::TURNS * 64;
+  const uint32_t buf = mem + F4Out<ROWS, SHARES>::TURNS * 64;
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     const uint4 w = ptx::ld_shared_v4(mem + i * 64 + q * 16);

@@ -6,7 +6,9 @@
 //           both products of its rows, a thread one row, and 32 neighbouring columns, a block of the quantisation, in its registers.
 //           One accumulator of 256 columns (a second does not fit beside the scales): the epilogue takes it into registers, 128 per thread,
 //           lets the next tile start, and works from there.
-//   GEMM-2  256 columns of W2 (M) x up to 192 rows (N, rounded up to 16: no padded rows), two accumulators.
+//   GEMM-2  256 columns of W2 (M) x up to 208 rows (N, rounded up to 16: no padded rows), two accumulators.  TMEM has room for the scales of four of its six
+//           stages: the UMMAs that read a slot's are waited for before it is filled again.  (With 192 rows and five stages, 4096 tokens, top-2 of 8 experts of 14336 x 4096: 240 us, 207 so; what bounds it are
+//           the bytes that tiles fetch, and 1024 rows are five tiles now instead of six.)
 // Two warps feed a stage, one its operands and one their scales: with five copies per stage one thread was busy for 400 of a stage's 512 cycles.
 // Pair protocol, barriers and the abort path are those of ffn_gemm2.cu; rank 0 issues every UMMA and copy of scales to TMEM.
 #include "ffn_fp4.cuh"
@@ -17,24 +19,28 @@ namespace tcmoe {
 namespace ffn {
 namespace {
 
-constexpr int EPI_WARPS = 8, TMA_WARP = EPI_WARPS, MMA_WARP = EPI_WARPS + 1, SF_WARP = EPI_WARPS + 2;
-constexpr int THREADS = (EPI_WARPS + 3) * 32;
 constexpr int W_BYTES = 128 * 128;                 // this CTA's 128 weight columns x 256 of K
 constexpr int SF_COLS = 24;                        // TMEM columns of a stage's scales
 constexpr int TABLE_BYTES = (3 * (MAX_E + 1) * 4 + 15) & ~15;
 constexpr uint32_t HINT = 4000;
 
 template <bool GLU> struct Geo {
+  // Eight: GEMM-1's hold 128 accumulator columns each in registers; GEMM-2's took 567 us with sixteen for 131072 rows of 1536 and 128 experts of 1536 x
+  // 4096, 540 with eight (the board is at its power limit).
+  static constexpr int EPI_WARPS = 8, SHARES = EPI_WARPS / 4;
+  static constexpr int TMA_WARP = EPI_WARPS, MMA_WARP = EPI_WARPS + 1, SF_WARP = EPI_WARPS + 2, THREADS = (EPI_WARPS + 3) * 32;
+  using Out = F4Out<F4_PAIR_ROWS2, SHARES>;   // GEMM-2
   static constexpr int TILE_ROWS = GLU ? F4_PAIR_ROWS1 : F4_PAIR_ROWS2;
   static constexpr int X_BYTES = 128 * TILE_ROWS / 2;
   static constexpr int STAGE_BYTES = W_BYTES + X_BYTES + 3 * F4_SF_BYTES;   // W, X, scales
-  static constexpr int NSTAGE = GLU ? 6 : 5;
+  static constexpr int NSTAGE = 6, SLOTS = GLU ? 6 : 4;   // stages, and those whose scales fit TMEM
+  static constexpr int MOST_ROWS = TILE_ROWS / 2;          // of a CTA
   static constexpr int BUFS = GLU ? 1 : 2;
   static constexpr int BUF_COLS = GLU ? 256 : F4_PAIR_ROWS2;
   static constexpr int SF_TMEM = BUFS * BUF_COLS;
   static constexpr int NUM_BARS = 2 * NSTAGE + 2 * BUFS;
-  static constexpr int SMEM_BYTES = 1024 + NSTAGE * STAGE_BYTES + NUM_BARS * 8 + 64 + TABLE_BYTES + (GLU ? 0 : EPI_WARPS * F4Out<F4_PAIR_ROWS2>::BYTES);
-  static_assert(SF_TMEM + NSTAGE * SF_COLS <= 512, "TMEM");
+  static constexpr int SMEM_BYTES = 1024 + NSTAGE * STAGE_BYTES + NUM_BARS * 8 + 64 + TABLE_BYTES + (GLU ? 0 : EPI_WARPS * Out::BYTES);
+  static_assert(SF_TMEM + SLOTS * SF_COLS <= 512, "TMEM");
   static_assert(SMEM_BYTES <= 232448, "shared memory of an SM");
   static_assert(STAGE_BYTES % 1024 == 0 && X_BYTES % 1024 == 0, "swizzle atoms");
 };
@@ -44,12 +50,12 @@ struct PairTile {
 };
 
 template <bool GLU>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Geo<GLU>::THREADS, 1)
 ffn_fp4_pair_kernel(const __grid_constant__ CUtensorMap map_wa, const __grid_constant__ CUtensorMap map_wb,
                     const __grid_constant__ CUtensorMap map_sfa, const __grid_constant__ CUtensorMap map_sfb,
                     const __grid_constant__ CUtensorMap map_sfx, const __grid_constant__ F4RowMaps xmaps, const F4Params p) {
   using G = Geo<GLU>;
-  constexpr int NSTAGE = G::NSTAGE;
+  constexpr int NSTAGE = G::NSTAGE, EPI_WARPS = G::EPI_WARPS, TMA_WARP = G::TMA_WARP, MMA_WARP = G::MMA_WARP, SF_WARP = G::SF_WARP;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + NSTAGE * G::STAGE_BYTES);
@@ -132,24 +138,24 @@ ffn_fp4_pair_kernel(const __grid_constant__ CUtensorMap map_wa, const __grid_con
   if (warp < EPI_WARPS) {
     // ================================ epilogue (both CTAs) ================================
     const int quarter = warp & 3, half = warp >> 2;
-    const uint32_t out_mem = ptx::smem_u32(tp_s) + TABLE_BYTES + (uint32_t)(warp * F4Out<F4_PAIR_ROWS2>::BYTES);   // GEMM-2
+    const uint32_t out_mem = ptx::smem_u32(tp_s) + TABLE_BYTES + (uint32_t)(warp * G::Out::BYTES);   // GEMM-2
     int tl = 0;
     PairTile t{}, next{};
-    float rw[(F4Out<F4_PAIR_ROWS2>::TURNS + 1) / 2];
+    float rw[(G::Out::TURNS + 1) / 2];
     if (cluster_id < total) {
       next = tile_of(cluster_id, 0);
-      if constexpr (!GLU) f4_fetch_weights<F4_PAIR_ROWS2>(p, next.row0, next.rows, half, lane, rw);
+      if constexpr (!GLU) f4_fetch_weights<F4_PAIR_ROWS2, G::SHARES>(p, next.row0, next.rows, half, lane, rw);
     }
     for (int w = cluster_id; w < total && !*abort_flag; w += num_clusters, ++tl) {
       t = next;
-      if constexpr (!GLU) f4_keep_weights<F4_PAIR_ROWS2>(rw, out_mem, lane);
+      if constexpr (!GLU) f4_keep_weights<F4_PAIR_ROWS2, G::SHARES>(rw, out_mem, lane);
       if (w + num_clusters < total) {
         next = tile_of(w + num_clusters, t.e);
-        if constexpr (!GLU) f4_fetch_weights<F4_PAIR_ROWS2>(p, next.row0, next.rows, half, lane, rw);
+        if constexpr (!GLU) f4_fetch_weights<F4_PAIR_ROWS2, G::SHARES>(p, next.row0, next.rows, half, lane, rw);
       }
       const int buf = GLU ? 0 : tl & 1;
       const uint32_t phase = GLU ? tl & 1 : (tl >> 1) & 1;
-      if (!ptx::mbar_wait_warp<false, GLU ? 0 : HINT>(tfull_bar(buf), phase, abort_flag, global_abort)) { timeout(1); break; }
+      if (!ptx::mbar_wait_warp<false, HINT>(tfull_bar(buf), phase, abort_flag, global_abort)) { timeout(1); break; }
       ptx::tc_fence_after();
       const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * G::BUF_COLS);
       if constexpr (GLU) {
@@ -173,10 +179,11 @@ ffn_fp4_pair_kernel(const __grid_constant__ CUtensorMap map_wa, const __grid_con
         for (int i = 0; i < 2; ++i) {
           float top = 0.f;
 #pragma unroll
-          for (int j = 0; j < 32; ++j) {
-            const float h = silu_mul(__uint_as_float(a[i][j]), __uint_as_float(b[i][j]));
-            top = fp4::max_nan(top, fabsf(h));
-            a[i][j] = __float_as_uint(h);
+          for (int j = 0; j < 32; j += 2) {
+            const float2 h = silu_mul2(__uint_as_float(a[i][j]), __uint_as_float(a[i][j + 1]), __uint_as_float(b[i][j]), __uint_as_float(b[i][j + 1]));
+            top = fp4::max_nan(top, fp4::max_nan(fabsf(h.x), fabsf(h.y)));
+            a[i][j] = __float_as_uint(h.x);
+            a[i][j + 1] = __float_as_uint(h.y);
           }
           const bool in = t.c0 * 128 + half * 64 + i * 32 < p.N;
           const uint32_t sb = in ? fp4::scale_byte(top) : 127u;
@@ -200,14 +207,14 @@ ffn_fp4_pair_kernel(const __grid_constant__ CUtensorMap map_wa, const __grid_con
           if (t.c0 + 1 == p.NC && (p.NC & 1)) *reinterpret_cast<uint16_t*>(sf + 512) = 0x7F7F;   // the chunk past the last column is part of a stage
         }
       } else {
-        // lane = column of this CTA's 128, TMEM column = row; the two warps of a quarter take turns
+        // lane = column of this CTA's 128, TMEM column = row; the warps of a quarter take turns
         const int col0 = (t.c0 + rank) * 128 + quarter * 32;
 #pragma unroll 1
-        for (int r0 = half * 16, i = 0; r0 < t.rows; r0 += 32, ++i) {
+        for (int r0 = half * 16, i = 0; r0 < t.rows; r0 += 16 * G::SHARES, ++i) {
           uint32_t a[16];
           ptx::tmem_ld16(taddr + r0, a);
           ptx::tmem_ld_wait_on(a);
-          f4_store_rows<G::TILE_ROWS>(p, a, out_mem, i, lane, t.row0 + r0, t.rows - r0, col0);
+          f4_store_rows<G::TILE_ROWS, G::SHARES>(p, a, out_mem, i, lane, t.row0 + r0, t.rows - r0, col0);
         }
         ptx::tc_fence_before();
         __syncwarp();
@@ -228,11 +235,12 @@ ffn_fp4_pair_kernel(const __grid_constant__ CUtensorMap map_wa, const __grid_con
         const int n = (t.rows + 15) & ~15, first = GLU ? rank * BM : rank * (n / 2);
         auto blocks32 = [&](int r) { return GLU ? (min(max(t.rows - r * BM, 0), BM) + 31) >> 5 : (n / 2 + 31) >> 5; };
         const int mine = blocks32(rank);
+        auto box_rows = [&](int blocks) { return min(32 * blocks, G::MOST_ROWS); };
         const int sets = t.rows > 128 ? 2 : 1;                                         // of the tile's scales
         const bool cols = GLU || t.c0 + rank < p.NC, both = GLU || t.c0 + 1 < p.NC;    // this CTA has weight columns; both have
         // of both CTAs: the leader announces them, the peer's copies only complete them
         const uint32_t bytes = scales ? ((GLU ? 4u : both ? 2u : 1u) + (GLU ? 1 : 2) * (uint32_t)sets) * F4_SF_BYTES
-                                      : (both ? 2u : 1u) * W_BYTES + (uint32_t)(blocks32(0) + blocks32(1)) * 32 * 128;
+                                      : (both ? 2u : 1u) * W_BYTES + (uint32_t)(box_rows(blocks32(0)) + box_rows(blocks32(1))) * 128;
         const int wc = t.e * p.NC + t.c0, set0 = 2 * t.tile;
         for (int kb = 0; kb < KB; ++kb) {
           if (!ptx::mbar_wait<false, HINT>(empty_bar(s), ph, abort_flag, global_abort)) {
@@ -264,8 +272,8 @@ ffn_fp4_pair_kernel(const __grid_constant__ CUtensorMap map_wa, const __grid_con
       const uint32_t base = __shfl_sync(0xFFFFFFFFu, smem_base, 0), tmem = __shfl_sync(0xFFFFFFFFu, tmem_base, 0);
       const uint64_t w_desc = desc_at(desc_base(16, 1024), base), x_desc = desc_at(desc_base(16, 1024), base + W_BYTES);
       const uint64_t sf_desc = scale_desc(base + W_BYTES + G::X_BYTES);
-      int s = 0, tl = 0, e = 0;
-      uint32_t ph = 0;
+      int s = 0, tl = 0, e = 0, slot = 0, old = 0, it = 0;   // old: the stage whose scales had the slot before
+      uint32_t ph = 0, old_ph = 0;
       bool ok = true;
       for (int w = cluster_id; ok && w < total && !*abort_flag; w += num_clusters, ++tl) {
         const int buf = GLU ? 0 : tl & 1;
@@ -279,10 +287,14 @@ ffn_fp4_pair_kernel(const __grid_constant__ CUtensorMap map_wa, const __grid_con
         const uint32_t id0 = idesc_f4(256, n, 0), id1 = idesc_f4(256, n, 2);
         for (int kb = 0; kb < KB; ++kb) {
           if (!ptx::mbar_wait_cluster<HINT>(full_bar(s), ph, abort_flag, global_abort)) { timeout(4); ok = false; break; }
+          if (G::SLOTS < NSTAGE && it++ >= G::SLOTS) {
+            if (!ptx::mbar_wait_cluster<HINT>(empty_bar(old), old_ph, abort_flag, global_abort)) { timeout(5); ok = false; break; }
+            if (++old == NSTAGE) { old = 0; old_ph ^= 1u; }
+          }
           ptx::tc_fence_after();
           if (elected) {
             const uint64_t so = (uint64_t)(s * (G::STAGE_BYTES >> 4));
-            const uint32_t sf = tmem + (uint32_t)(G::SF_TMEM + s * SF_COLS);
+            const uint32_t sf = tmem + (uint32_t)(G::SF_TMEM + slot * SF_COLS);
             // Shared memory: three sets of two chunks.  TMEM, columns: GEMM-1 rows 0 4, W1 | W3 of one 128 of K side by side 8 12, 16 20;
             // GEMM-2 the two sets of rows side by side 0 4, 8 12, W2 16 20.
             constexpr int at[6] = {0, GLU ? 4 : 8, GLU ? 8 : 4, GLU ? 16 : 12, GLU ? 12 : 16, 20};
@@ -297,6 +309,7 @@ ffn_fp4_pair_kernel(const __grid_constant__ CUtensorMap map_wa, const __grid_con
             ptx::umma_commit_both(empty_bar(s));   // free the stage in both CTAs once these UMMAs have read it
           }
           if (++s == NSTAGE) { s = 0; ph ^= 1u; }
+          if (++slot == G::SLOTS) slot = 0;
         }
         if (ok && elected) ptx::umma_commit_both(tfull_bar(buf));   // accumulator complete, both CTAs
       }
@@ -327,7 +340,7 @@ cudaError_t launch(const F4Params& p, const void* wa, const void* wb, const void
     int clusters = 0;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(sm_count() & ~1);
-    cfg.blockDim = dim3(THREADS);
+    cfg.blockDim = dim3(G::THREADS);
     cfg.dynamicSmemBytes = G::SMEM_BYTES;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeClusterDimension;
@@ -351,9 +364,9 @@ cudaError_t launch(const F4Params& p, const void* wa, const void* wb, const void
       !make_scale_map(&m_sx, p.sfx, row_sets * fp4::chunks(p.K)))
     return cudaErrorInvalidValue;
   for (int i = 0; i < 4; ++i)
-    if (!make_act_map(&x.m[i], rows, n_rows, p.K / 2, true, 32 * (i + 1))) return cudaErrorInvalidValue;
+    if (!make_act_map(&x.m[i], rows, n_rows, p.K / 2, true, min(32 * (i + 1), G::MOST_ROWS))) return cudaErrorInvalidValue;
   ProfileScope prof(GLU ? KID_GEMM1 : KID_GEMM2, st);
-  return launch_pdl(ffn_fp4_pair_kernel<GLU>, dim3(grid), dim3(THREADS), G::SMEM_BYTES, st, m_a, m_b, m_sa, m_sb, m_sx, x, p);
+  return launch_pdl(ffn_fp4_pair_kernel<GLU>, dim3(grid), dim3(G::THREADS), G::SMEM_BYTES, st, m_a, m_b, m_sa, m_sb, m_sx, x, p);
 }
 
 }  // namespace
