@@ -404,9 +404,11 @@ cudaError_t launch_form(const F4Params& p, const void* wa, const void* wb, const
     attr_set[dev].store(true, std::memory_order_release);
   }
   CUtensorMap m_a, m_b;
-  F4RowMaps x;
-  if (!make_weight_map_fp8(&m_a, wa, p.E, p.N, p.K / 2, 128) || !make_weight_map_fp8(&m_b, wb, p.E, p.N, p.K / 2, 128)) return cudaErrorInvalidValue;
-  for (int i = 0; i < 4; ++i)
+  F4RowMaps x{};
+  if (!make_weight_map_fp8(&m_a, wa, p.E, p.N, p.K / 2, 128)) return cudaErrorInvalidValue;
+  m_b = m_a;
+  if (GLU && !make_weight_map_fp8(&m_b, wb, p.E, p.N, p.K / 2, 128)) return cudaErrorInvalidValue;
+  for (int i = 0; i < F4_ROWS / 32; ++i)
     if (!make_act_map(&x.m[i], rows, n_rows, p.K / 2, true, 32 * (i + 1))) return cudaErrorInvalidValue;
   ProfileScope prof(GLU ? KID_GEMM1 : KID_GEMM2, st);
   return launch_pdl(ffn_fp4_kernel<GLU, SHARE>, dim3(min(sm_count(), F4_CTAS)), dim3(THREADS), SMEM_BYTES, st, m_a, m_b, x, p);

@@ -359,10 +359,12 @@ cudaError_t launch(const F4Params& p, const void* wa, const void* wb, const void
   CUtensorMap m_a, m_b, m_sa, m_sb, m_sx;
   F4RowMaps x;
   const long long w_chunks = (long long)p.E * p.NC * fp4::chunks(p.K);
-  if (!make_weight_map_fp8(&m_a, wa, p.E, p.N, p.K / 2, 128) || !make_weight_map_fp8(&m_b, wb, p.E, p.N, p.K / 2, 128) ||
-      !make_scale_map(&m_sa, p.sfa, w_chunks) || !make_scale_map(&m_sb, p.sfb, w_chunks) ||
+  if (!make_weight_map_fp8(&m_a, wa, p.E, p.N, p.K / 2, 128) || !make_scale_map(&m_sa, p.sfa, w_chunks) ||
       !make_scale_map(&m_sx, p.sfx, row_sets * fp4::chunks(p.K)))
     return cudaErrorInvalidValue;
+  m_b = m_a;
+  m_sb = m_sa;
+  if (GLU && (!make_weight_map_fp8(&m_b, wb, p.E, p.N, p.K / 2, 128) || !make_scale_map(&m_sb, p.sfb, w_chunks))) return cudaErrorInvalidValue;
   for (int i = 0; i < 4; ++i)
     if (!make_act_map(&x.m[i], rows, n_rows, p.K / 2, true, min(32 * (i + 1), G::MOST_ROWS))) return cudaErrorInvalidValue;
   ProfileScope prof(GLU ? KID_GEMM1 : KID_GEMM2, st);

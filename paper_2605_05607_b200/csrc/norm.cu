@@ -159,17 +159,17 @@ __global__ void __launch_bounds__(WARPS == 1 ? 256 : WARPS * 32) rmsnorm_backwar
   __shared__ float part[2][WARPS];
   grid_dependency_sync();
   const int lane = WARPS == 1 ? threadIdx.x & 31 : threadIdx.x, team = WARPS == 1 ? threadIdx.x >> 5 : 0, n_vec = a.vec_per_row;
-  const int r0 = blockIdx.x * TEAMS + team, step = gridDim.x * TEAMS;
+  const long long r0 = (long long)blockIdx.x * TEAMS + team, step = (long long)gridDim.x * TEAMS;   // sums with them pass 32 bits at the largest row counts
   uint4* ring = ring_s + team * STAGES * STREAMS * n_vec;
   const uint4* const from[3] = {a.dy, a.s, a.dres};
-  auto fetch = [&](int r, int stage) {
+  auto fetch = [&](long long r, int stage) {
     if (r < a.rows) {
 #pragma unroll
       for (int q = 0; q < STREAMS; ++q)
 #pragma unroll
         for (int i = 0; i < KEEP; ++i) {
           const int v = lane + LANES * i;
-          if (v < n_vec) ptx::cp_async_16(ptx::smem_u32(ring + (stage * STREAMS + q) * n_vec + v), from[q] + (long long)r * n_vec + v, 16);
+          if (v < n_vec) ptx::cp_async_16(ptx::smem_u32(ring + (stage * STREAMS + q) * n_vec + v), from[q] + r * n_vec + v, 16);
         }
     }
     ptx::cp_async_commit();
@@ -186,7 +186,7 @@ __global__ void __launch_bounds__(WARPS == 1 ? 256 : WARPS * 32) rmsnorm_backwar
   int flip = 0, stage = 0;
   const float n = (float)(n_vec * VEC);
   float rstd = r0 < a.rows ? __ldg(a.rstd + r0) : 0.f;
-  for (int r = r0; r < a.rows; r += step) {
+  for (long long r = r0; r < a.rows; r += step) {
     const float next = r + step < a.rows ? __ldg(a.rstd + r + step) : 0.f;
     ptx::cp_async_wait<STAGES - 1>();   // this row's copies of this thread
     uint4 dyv[KEEP], sv[KEEP], kv[SKIP ? KEEP : 1];
@@ -235,7 +235,7 @@ __global__ void __launch_bounds__(WARPS == 1 ? 256 : WARPS * 32) rmsnorm_backwar
           const float g = (dy[j] * w[i][j] - (s[j] * rstd) * mean) * rstd;
           s[j] = SKIP ? g + k[j] : g;
         }
-        a.dx[(long long)r * n_vec + v] = pack8(s);
+        a.dx[r * n_vec + v] = pack8(s);
       }
     }
     rstd = next;

@@ -159,6 +159,30 @@ def check_ffn(shape, ws, lay, xg, w, wt, weighted=True):
     return o
 
 
+# long walks over K with fewer tiles than SMs: their stages are shared out among the CTAs, parts of tiles are added up
+@pytest.mark.parametrize("counts", [(1,), (2, 3), (0, 16, 17), (33, 1, 95), (96,), (60, 80)], ids=str)
+@pytest.mark.parametrize("d,f", [(512, 4096), (4096, 512), (2080, 4640)])
+def test_expert_ffn_fp4_of_shared_tiles(counts, d, f):
+    shape, ws, lay, x, xg, idx, w, wt = routed(counts, d=d, f=f, seed=sum(counts) + d)
+    o = check_ffn(shape, ws, lay, xg, w, wt)
+    args = (shape, *rows_fp4(xg), lay, w, *quantised(wt))
+    for _ in range(5):                                      # the parts are added in a fixed order, whoever is last
+        again = torch.full_like(o, 7.0)
+        B.moe_expert_ffn_fp4(*args, again, ws)
+        assert torch.equal(again, o)
+
+
+def test_expert_ffn_fp4_most_experts_and_no_token():
+    shape, ws, lay, x, xg, idx, w, wt = routed((300, 1024), 4, 64, 32, 5, 8)
+    check_ffn(shape, ws, lay, xg, w, wt)
+    cfg = H.synth.MoEConfig("fp4-none", T=0, d=64, f=32, E=8, k=2, G=2)
+    sh = B.make_shape(cfg)
+    y = torch.full((1, 64), 7.0, device="cuda").bfloat16()
+    wg, q = torch.zeros(64, 8, device="cuda"), quantised([v[:8].contiguous() for v in wt])
+    B.moe_layer_fp4(sh, x, wg, None, *q, y, B.alloc_workspace(sh))
+    assert (y == 7).all()
+
+
 SMALL = [(1,), (1, 0, 3), (16, 17), (33, 1, 95, 96), (97, 192, 193), (0, 0, 5), (300,), (31, 32, 64, 65, 128, 129)]
 
 
