@@ -176,12 +176,16 @@ __global__ void __launch_bounds__(WARPS == 1 ? 256 : WARPS * 32) rmsnorm_backwar
   };
 #pragma unroll
   for (int i = 0; i < STAGES; ++i) fetch(r0 + i * step, i);
-  float dw[KEEP][VEC], w[KEEP][VEC];
+  float2 dw[KEEP][VEC / 2], w[KEEP][VEC / 2];
 #pragma unroll
   for (int i = 0; i < KEEP; ++i) {
+    float f[VEC] = {};
+    if (lane + LANES * i < n_vec) load_w(a.w, a.w32, lane + LANES * i, f);
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) dw[i][j] = 0.f;
-    if (lane + LANES * i < n_vec) load_w(a.w, a.w32, lane + LANES * i, w[i]);
+    for (int j = 0; j < VEC; j += 2) {
+      dw[i][j / 2] = make_float2(0.f, 0.f);
+      w[i][j / 2] = make_float2(f[j], f[j + 1]);
+    }
   }
   int flip = 0, stage = 0;
   const float n = (float)(n_vec * VEC);
@@ -190,7 +194,7 @@ __global__ void __launch_bounds__(WARPS == 1 ? 256 : WARPS * 32) rmsnorm_backwar
     const float next = r + step < a.rows ? __ldg(a.rstd + r + step) : 0.f;
     ptx::cp_async_wait<STAGES - 1>();   // this row's copies of this thread
     uint4 dyv[KEEP], sv[KEEP], kv[SKIP ? KEEP : 1];
-    float dot = 0.f;
+    float2 dots = make_float2(0.f, 0.f);   // sum of dy * s * w, over even and odd columns
 #pragma unroll
     for (int i = 0; i < KEEP; ++i) {
       const int v = lane + LANES * i;
@@ -202,13 +206,14 @@ __global__ void __launch_bounds__(WARPS == 1 ? 256 : WARPS * 32) rmsnorm_backwar
         unpack8(dyv[i], dy);
         unpack8(sv[i], s);
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-          const float t = dy[j] * (s[j] * rstd);
-          dw[i][j] += t;
-          dot = fmaf(t, w[i][j], dot);
+        for (int j = 0; j < VEC; j += 2) {
+          const float2 t = __fmul2_rn(make_float2(dy[j], dy[j + 1]), make_float2(s[j], s[j + 1]));
+          dw[i][j / 2] = __ffma2_rn(t, make_float2(rstd, rstd), dw[i][j / 2]);
+          dots = __ffma2_rn(t, w[i][j / 2], dots);
         }
       }
     }
+    float dot = dots.x + dots.y;
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, off);
     if (WARPS > 1) {   // two buffers: the next row's sums do not overwrite what a slow warp still reads
@@ -221,7 +226,7 @@ __global__ void __launch_bounds__(WARPS == 1 ? 256 : WARPS * 32) rmsnorm_backwar
     }
     fetch(r + STAGES * step, stage);   // the stage's values are in registers (their sum has been used)
     if (++stage == STAGES) stage = 0;
-    const float mean = dot / n;
+    const float c = -(dot / n) * rstd * rstd;   // dx = rstd * (dy * w + c * s) + dres
 #pragma unroll
     for (int i = 0; i < KEEP; ++i) {
       const int v = lane + LANES * i;
@@ -231,9 +236,12 @@ __global__ void __launch_bounds__(WARPS == 1 ? 256 : WARPS * 32) rmsnorm_backwar
         unpack8(sv[i], s);
         if (SKIP) unpack8(kv[i], k);
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-          const float g = (dy[j] * w[i][j] - (s[j] * rstd) * mean) * rstd;
-          s[j] = SKIP ? g + k[j] : g;
+        for (int j = 0; j < VEC; j += 2) {
+          const float2 g = __fmul2_rn(make_float2(dy[j], dy[j + 1]), w[i][j / 2]), s2 = make_float2(s[j], s[j + 1]), c2 = make_float2(c, c);
+          const float2 t = __ffma2_rn(s2, c2, g), r2 = make_float2(rstd, rstd);
+          const float2 o = SKIP ? __ffma2_rn(t, r2, make_float2(k[j], k[j + 1])) : __fmul2_rn(t, r2);
+          s[j] = o.x;
+          s[j + 1] = o.y;
         }
         a.dx[r * n_vec + v] = pack8(s);
       }
@@ -249,7 +257,7 @@ __global__ void __launch_bounds__(WARPS == 1 ? 256 : WARPS * 32) rmsnorm_backwar
       const int v = lane + LANES * i;
       if (v < n_vec)
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) sums[(team * n_vec + v) * VEC + j] = dw[i][j];
+        for (int j = 0; j < VEC / 2; ++j) reinterpret_cast<float2*>(sums)[(team * n_vec + v) * VEC / 2 + j] = dw[i][j];
     }
     __syncthreads();
     for (int c = threadIdx.x; c < n_vec * VEC; c += 256) {
@@ -265,8 +273,8 @@ __global__ void __launch_bounds__(WARPS == 1 ? 256 : WARPS * 32) rmsnorm_backwar
     const int v = lane + LANES * i;
     if (v < n_vec) {
       float4* out = reinterpret_cast<float4*>(a.part + (long long)blockIdx.x * n_vec * VEC) + 2 * v;
-      out[0] = make_float4(dw[i][0], dw[i][1], dw[i][2], dw[i][3]);
-      out[1] = make_float4(dw[i][4], dw[i][5], dw[i][6], dw[i][7]);
+      out[0] = make_float4(dw[i][0].x, dw[i][0].y, dw[i][1].x, dw[i][1].y);
+      out[1] = make_float4(dw[i][2].x, dw[i][2].y, dw[i][3].x, dw[i][3].y);
     }
   }
 }
@@ -328,7 +336,7 @@ cudaError_t launch_norm_bwd(const NormBwdArgs& a, int* parts, cudaStream_t st) {
   if (cols <= 1024) return go(rmsnorm_backward_kernel<4, 1, 3, SKIP>, 256, 3, 8);
   if (cols <= 2048) return go(rmsnorm_backward_kernel<1, 8, 4, SKIP>, 256, 4);
   if (cols <= 4096) return go(rmsnorm_backward_kernel<1, 16, 4, SKIP>, 512, 4);
-  if (cols <= 8192) return go(rmsnorm_backward_kernel<2, 16, 3, SKIP>, 512, 3);
+  if (cols <= 8192) return go(rmsnorm_backward_kernel<2, 16, SKIP ? 3 : 4, SKIP>, 512, SKIP ? 3 : 4);   // 8000 of 7168 without dres, three stages 75 us, four 70
   return go(rmsnorm_backward_kernel<4, 16, 2, SKIP>, 512, 2);   // NORM_COLS
 }
 
