@@ -54,9 +54,9 @@ __device__ __forceinline__ uint32_t codes8(const float (&f)[8], float inv) {
     c |= (uint32_t)__nv_cvt_float2_to_fp4x2(make_float2(f[2 * q] * inv, f[2 * q + 1] * inv), __NV_E2M1, cudaRoundNearest) << (8 * q);
   return c;
 }
-// the code of one (scaled) value
-__device__ __forceinline__ uint32_t code(float v) {
-  return (uint32_t)__nv_cvt_float2_to_fp4x2(make_float2(v, 0.f), __NV_E2M1, cudaRoundNearest) & 15u;
+// the codes of two (scaled) values, the first in the low half
+__device__ __forceinline__ uint32_t code2(float a, float b) {
+  return (uint32_t)__nv_cvt_float2_to_fp4x2(make_float2(a, b), __NV_E2M1, cudaRoundNearest);
 }
 // An 8 x 8 transpose of 4-bit pieces over eight neighbouring lanes: piece i of lane l becomes piece l of lane i.
 __device__ __forceinline__ uint32_t transpose8(uint32_t v, int lane) {
