@@ -441,12 +441,13 @@ long long fp4_row_sets(const Shape& s) {
   return one > two ? one : two;
 }
 
-// CTA pairs from 112 rows per expert on.  FFN on single CTAs / pairs, us, rows per expert in brackets: 3200 tokens, top-4 of 128 x 2048 x 1024 (100)
-// 161 / 139, 1777 skewed, top-4 of 64 x 2880 x 2880 (111) 246 / 270, 450, top-2 of 8 x 4096 x 4096 (112) 72 / 69, 1000 skewed, top-4 of
-// 32 x 1024 x 1024 (125) 52 / 41, 4096, top-2 of 64 x 2048 x 2048 (128) 174 / 134, 800, top-2 of 8 x 2048 x 7168 (200) 99 / 72, 3600 skewed on
-// 16 x 4096 x 1536 (225) 87 / 81.  (Both forms side by side, each for the experts of its kind, gained nothing where routing is skewed,
-// 246 / 243, and lost where tiles are few: 400 skewed, top-2 of 8 x 4096 x 4096, 69 / 85.)
-static bool fp4_pairs(const Shape& s) { return (long long)s.T * s.k >= 112ll * s.E; }
+// CTA pairs from 128 rows per expert on.  FFN on single CTAs / pairs, us, rows per expert in brackets: 1500 skewed tokens, top-2 of 64 x 2048 x 2048 (47)
+// 97 / 117, 3000, top-2 of 64 x 2048 x 2048 (94) 108 / 120, 3200, top-4 of 128 x 2048 x 1024 (100) 133 / 133, 3318 on 32 x 1888 x 7168 (104) 217 / 198, 1777
+// skewed, top-4 of 64 x 2880 x 2880 (111) 225 / 252, 450, top-2 of 8 x 4096 x 4096 (112) 66 / 66, 1000 skewed, top-4 of 32 x 1024 x 1024 (125) 37 / 41,
+// 4096, top-2 of 64 x 2048 x 2048 (128) 135 / 128, 2900, top-2 of 32 x 2880 x 2880 (181) 156 / 135, 800, top-2 of 8 x 2048 x 7168 (200) 77 / 67, 3600
+// skewed on 16 x 4096 x 1536 (225) 81 / 79.  (Both forms side by side, each for the experts of its kind, gained nothing where
+// routing is skewed and lost where tiles are few.)
+static bool fp4_pairs(const Shape& s) { return (long long)s.T * s.k >= 128ll * s.E; }
 
 // Whether a product's tiles (at most row_tiles * ceil(N / width)) are shared.  A CTA streams at most 63 KB/us, all together 6.5 TB/s: tiles that leave SMs
 // idle take KB * 0.55 us whole, tiles * KB * 0.0052 us shared and then about 4 us for their parts.
