@@ -14,7 +14,7 @@
 // One persistent CTA per SM takes every 148th tile.  SHARE, for layers with fewer tiles than SMs: the stages of all tiles, one tile after the other, are
 // divided evenly among the CTAs.  A tile that several of them share leaves as fp32 parts; per epilogue warp, the one that writes the last part adds
 // them up, in the order of K whoever is last, puts the sums back into its accumulator and goes on as if they were its own.  GEMM-2 of one token,
-// top-2 of 4096 x 14336 (32 tiles): XXX us.  (With all layers divided this way, 64 tokens, top-8 of 128 experts of 4096 x 1536, took
+// top-2 of 4096 x 14336 (32 tiles): 31 us, 22 so.  (With all layers divided this way, 64 tokens, top-8 of 128 experts of 4096 x 1536, took
 // 218 us instead of 211: neighbouring CTAs no longer stream neighbouring columns.  A form of its own, because the larger code alone costs the others
 // up to 4 us: instructions that are missed in the cache wait behind the weights that are on their way.)
 //
@@ -473,7 +473,8 @@ cudaError_t launch_expert_ffn_fp4(const Shape& s, const FfnArgs& a, const Fp4Arg
   const bool pairs = fp4_pairs(s);
   const int rows1 = pairs ? ffn::F4_PAIR_ROWS1 : ffn::F4_ROWS, rows2 = pairs ? ffn::F4_PAIR_ROWS2 : ffn::F4_ROWS;
   float* row_w = a.topk_w != nullptr ? q.row_w : nullptr;
-  const int chunk = P >= 8 * 64 * sm_count() ? 8 : 1;   // rows per warp: one as long as all of them are resident at once
+  // rows per warp: one as long as all of them are resident at once; 131072 rows of 4096, us with 1 / 2 / 4 / 8 / 16: 122 / 94 / 89 / 95 / 116
+  const int chunk = P >= 8 * 64 * sm_count() ? 4 : 1;
   cudaError_t e = launch_pdl(ffn::fp4_sort_kernel, dim3((unsigned)((P + 8 * chunk - 1) / (8 * chunk))), dim3(256), 0, st, static_cast<const uint4*>(a.a_src),
                              q.sx, a.a_rows, a.gather_idx, a.gather_div, a.expert_offsets, s.E, s.d, P, rows1, chunk, static_cast<uint4*>(a.xs), q.sfx,
                              a.topk_w, a.row_pair, row_w, q.arrived, (int)(fp4_arrived_bytes(s) / 4), a.status);

@@ -55,7 +55,7 @@ __device__ __forceinline__ uint64_t scale_desc(uint32_t smem_addr) {
 __device__ __forceinline__ void f4_load_offsets(const int32_t* expert_offsets, int E, int* eoff) {
   for (int i = threadIdx.x; i <= E; i += blockDim.x) eoff[i] = __ldcg(expert_offsets + i);
 }
-// silu(a) * b = a b / (1 + 2^(-a log2 e)) of two values: products and sums two at a time (f32x2)
+// silu(a) * b = (a / (1 + 2^(-a log2 e))) * b of two values: products and sums two at a time (f32x2)
 __device__ __forceinline__ float2 silu_mul2(float a0, float a1, float b0, float b1) {
   float2 h;
   asm("{\n\t.reg .b64 a, b, t, c;\n\t.reg .f32 x, y;\n\t"
@@ -64,7 +64,7 @@ __device__ __forceinline__ float2 silu_mul2(float a0, float a1, float b0, float 
       "mov.b64 {x, y}, t;\n\tex2.approx.ftz.f32 x, x;\n\tex2.approx.ftz.f32 y, y;\n\tmov.b64 t, {x, y};\n\t"
       "mov.b64 c, {%7, %7};\n\tadd.rn.f32x2 t, t, c;\n\t"
       "mov.b64 {x, y}, t;\n\trcp.approx.ftz.f32 x, x;\n\trcp.approx.ftz.f32 y, y;\n\tmov.b64 t, {x, y};\n\t"
-      "mul.rn.f32x2 a, a, b;\n\tmul.rn.f32x2 t, a, t;\n\tmov.b64 {%0, %1}, t;\n\t}"
+      "mul.rn.f32x2 t, a, t;\n\tmul.rn.f32x2 t, t, b;\n\tmov.b64 {%0, %1}, t;\n\t}"
       : "=f"(h.x), "=f"(h.y)
       : "f"(a0), "f"(a1), "f"(b0), "f"(b1), "f"(-1.4426950408889634f), "f"(1.f));
   return h;

@@ -7,8 +7,8 @@
 //           One accumulator of 256 columns (a second does not fit beside the scales): the epilogue takes it into registers, 128 per thread,
 //           lets the next tile start, and works from there.
 //   GEMM-2  256 columns of W2 (M) x up to 208 rows (N, rounded up to 16: no padded rows), two accumulators.  TMEM has room for the scales of four of its six
-//           stages: the UMMAs that read a slot's are waited for before it is filled again.  (With 192 rows and five stages, 4096 tokens, top-2 of 8 experts of 14336 x 4096: 240 us, 207 so; what bounds it are
-//           the bytes that tiles fetch, and 1024 rows are five tiles now instead of six.)
+//           stages: the UMMAs that read a slot's are waited for before it is filled again.  (With 192 rows and five stages, 4096 tokens, top-2 of 8 experts
+//           of 14336 x 4096: 240 us, 207 so; 1024 rows are five tiles instead of six.)
 // Two warps feed a stage, one its operands and one their scales: with five copies per stage one thread was busy for 400 of a stage's 512 cycles.
 // Pair protocol, barriers and the abort path are those of ffn_gemm2.cu; rank 0 issues every UMMA and copy of scales to TMEM.
 #include "ffn_fp4.cuh"

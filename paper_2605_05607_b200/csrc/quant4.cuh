@@ -15,6 +15,12 @@ __device__ __forceinline__ float max_nan(float a, float b) {   // NaN if either 
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
   return m;
 }
+// larger magnitudes of two pairs of bf16, NaN if either is
+__device__ __forceinline__ uint32_t max_nan2(uint32_t magnitudes, uint32_t pair) {
+  uint32_t m;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(m) : "r"(magnitudes), "r"(pair & 0x7FFF7FFFu));
+  return m;
+}
 // E8M0 byte of a block whose largest magnitude is `top`: floor(log2(top)) is the exponent field, and subnormals (field 0) lie below the lowest scale
 __device__ __forceinline__ uint32_t scale_byte(float top) {
   const uint32_t field = __float_as_uint(top) >> 23;

@@ -354,3 +354,77 @@ def test_expert_ffn_fp4_reports_a_source_row_out_of_range():
     B.moe_expert_ffn_fp4(shape, *rows_fp4(xg), lay, w, *quantised(wt), o, ws)
     st = B.moe_status(ws)
     assert st[0] == B.MOE_DEV_INDEX_OUT_OF_RANGE and st[2] == 30 and st[3] == 4
+
+
+class Fenced:
+    """Buffers of exactly the size that the interface asks for, in the middle of bytes that nothing may touch."""
+
+    def __init__(self):
+        self.all = []
+
+    def __call__(self, nbytes, dtype=torch.uint8, shape=None, fill=0):
+        pad = 1 << 16
+        raw = torch.full((nbytes + 2 * pad,), 0xC5, dtype=torch.uint8, device="cuda")
+        assert raw.data_ptr() % 128 == 0
+        raw[pad:pad + nbytes] = fill
+        self.all.append((raw, pad, nbytes))
+        t = raw[pad:pad + nbytes].view(dtype)
+        return t if shape is None else t.view(shape)
+
+    def check(self):
+        torch.cuda.synchronize()
+        for raw, pad, n in self.all:
+            assert (raw[:pad] == 0xC5).all() and (raw[pad + n:] == 0xC5).all()
+
+
+@pytest.mark.parametrize("T,E,k,d,f,zipf", [(1, 8, 2, 2048, 4096, 0), (3, 64, 8, 96, 64, 0), (97, 4, 1, 288, 544, 0), (129, 1, 1, 32, 32, 0), (700, 4, 2, 288, 160, 1),
+                                            (2000, 16, 1, 64, 96, 1), (640, 128, 5, 32, 32, 1), (1537, 3, 3, 96, 1056, 0), (500, 2, 1, 160, 288, 0)])
+def test_fp4_stays_inside_its_buffers(T, E, k, d, f, zipf):
+    g = torch.Generator(device="cuda").manual_seed(T)
+    idx = (torch.rand(T, E, generator=g, device="cuda") - zipf * torch.arange(E, device="cuda") / E).topk(k, dim=1).indices.int().contiguous()
+    shape, buf = B.MoEShape(T, d, f, E, k, 1, 0, 0), Fenced()
+    lay, ws = B.alloc_layout(shape), buf(B.moe_workspace_bytes(shape))
+    x = torch.randn(T, d, generator=g, device="cuda").bfloat16()
+    B.moe_dispatch(shape, None, idx, lay, None, ws)
+    w = torch.rand(T, k, generator=g, device="cuda") + 0.1
+    q, refs = [], []
+    for K, N in ((d, f), (d, f), (f, d)):
+        v = torch.randn(E, K, N, generator=g, device="cuda").div(K ** 0.5).bfloat16()
+        q += [buf(E * N * K // 2, shape=(E, N, K // 2)), buf(B.moe_fp4_scale_bytes(E, K, N))]
+        B.moe_quantize_weights_fp4(v, *q[-2:])
+        back = buf(E * K * N * 2, torch.bfloat16, (E, K, N))
+        B.moe_dequantize_weights_fp4(*q[-2:], back)
+        refs += Q.quantize_weights(f64(v))
+    xq, sx = buf(T * d // 2, shape=(T, d // 2)), buf(T * d // 32, shape=(T, d // 32))
+    B.moe_quantize_rows_fp4(x, xq, sx)
+    B.moe_dequantize_rows_fp4(xq, sx, buf(T * d * 2, torch.bfloat16, (T, d)))
+    o = buf(T * k * d * 2, torch.bfloat16, (T * k, d))
+    ws[64:] = 0xEE                                           # nothing in the workspace but the status block has to start at zero
+    B.moe_expert_ffn_fp4(shape, xq, sx, lay, w, *q, o, ws)
+    assert B.moe_status(ws)[0] == 0
+    buf.check()
+    n = T * k
+    hl = {"expert_offsets": lay.expert_offsets[: E + 1].cpu().numpy(), "row_pair": lay.row_pair.cpu().numpy()[:n], "row_src": lay.row_src.cpu().numpy()[:n]}
+    ref, tol = Q.expert_ffn_fp4(*Q.quantize_rows(f64(x)), hl, w.cpu().numpy(), *refs)
+    got = f64(o)
+    assert (np.abs(got - ref) <= tol + 2.0 ** -8 * (np.abs(ref) + tol)).all()
+    # the same through the layer, with its own routing
+    wg, y = torch.randn(d, E, generator=g, device="cuda") * 0.1, buf(T * d * 2, torch.bfloat16, (T, d), fill=0xFF)
+    B.moe_layer_fp4(shape, x, wg, None, *q, y, ws)
+    assert B.moe_status(ws)[0] == 0 and torch.isfinite(y.float()).all()
+    buf.check()
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 8), (3, 520), (700, 1024), (61, 2056), (9, 16384), (2500, 4096)])
+def test_norm_stays_inside_its_buffers(rows, cols):
+    buf = Fenced()
+    bf = lambda: buf(rows * cols * 2, torch.bfloat16, (rows, cols))   # noqa: E731
+    x, r, dy = (torch.randn(rows, cols, device="cuda").bfloat16() for _ in range(3))
+    w = torch.ones(cols, device="cuda")
+    y, s, q = bf(), bf(), buf(rows * cols, shape=(rows, cols))
+    sc, rs = buf(rows * 4, torch.float32), buf(rows * 4, torch.float32)
+    B.moe_rmsnorm(x, w, 1e-6, y=y, residual=r, res_out=s, yq=q, scale=sc, rstd=rs)
+    dx, dw = bf(), buf(cols * 4, torch.float32)
+    B.moe_rmsnorm_backward(dy, s, w, rs, dx, dw, buf(B.moe_rmsnorm_backward_workspace_bytes(rows, cols), fill=0xEE), dres=r)
+    buf.check()
+    assert torch.isfinite(dx.float()).all() and torch.isfinite(dw).all()
