@@ -151,11 +151,14 @@ struct NormBwdArgs {
 
 // Rows come through shared memory, STAGES of them on their way per block: every thread copies (cp.async) the vectors that it will use itself, so it waits
 // for its own copies and for nobody.  Loaded into registers instead, a row at a time, 8192 rows of 4096 with dres took 67 us, 49 so.
-// WARPS warps per row; WARPS == 1: eight rows per block, whose dw are joined at the end (16000 rows of 512 with two warps per row: 35.9 us, 18.6 so).
-template <int KEEP, int WARPS, int STAGES, bool SKIP>
-__global__ void __launch_bounds__(WARPS == 1 ? 256 : WARPS * 32) rmsnorm_backward_kernel(const NormBwdArgs a) {
+// WARPS warps per row, or (FIT) as many as the block has; WARPS == 1: eight rows per block, whose dw are joined at the end (16000 rows of 512 with two warps per row: 35.9 us, 18.6 so).
+// Without dres two blocks of 512 fit an SM by their shared memory, so they are held to the registers for it (64, 82 left alone: 8370 rows of 7168 103 us, 70
+// so); with dres shared memory leaves room for one, and fewer registers cost (8370 of 7168 79 us, 116 so).
+template <int KEEP, int WARPS, int STAGES, bool SKIP, bool FIT>
+__global__ void __launch_bounds__(WARPS == 1 ? 256 : WARPS * 32, WARPS == 16 && KEEP <= 2 && !SKIP ? 2 : 0) rmsnorm_backward_kernel(const NormBwdArgs a) {
   extern __shared__ __align__(16) uint4 ring_s[];   // per row of the block: [STAGES][dy, s, dres][vec_per_row]
-  constexpr int LANES = WARPS * 32, STREAMS = SKIP ? 3 : 2, TEAMS = WARPS == 1 ? 8 : 1;
+  constexpr int STREAMS = SKIP ? 3 : 2, TEAMS = WARPS == 1 ? 8 : 1;
+  const int LANES = FIT ? blockDim.x : WARPS * 32;
   __shared__ float part[2][WARPS];
   grid_dependency_sync();
   const int lane = WARPS == 1 ? threadIdx.x & 31 : threadIdx.x, team = WARPS == 1 ? threadIdx.x >> 5 : 0, n_vec = a.vec_per_row;
@@ -221,7 +224,8 @@ __global__ void __launch_bounds__(WARPS == 1 ? 256 : WARPS * 32) rmsnorm_backwar
       __syncthreads();
       dot = 0.f;
 #pragma unroll
-      for (int i = 0; i < WARPS; ++i) dot += part[flip][i];
+      for (int i = 0; i < WARPS; ++i)
+        if (!FIT || i * 32 < LANES) dot += part[flip][i];
       flip ^= 1;
     }
     fetch(r + STAGES * step, stage);   // the stage's values are in registers (their sum has been used)
@@ -328,16 +332,24 @@ cudaError_t launch_norm_bwd(const NormBwdArgs& a, int* parts, cudaStream_t st) {
       const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
       if (e != cudaSuccess) return e;
     }
-    const int per_sm = max(1, min(min(4, 1024 / threads), 226 * 1024 / (smem + 1280)));
+    const int per_sm = max(1, min(min(4, 1152 / threads), 226 * 1024 / (smem + 1280)));
     *parts = min(min((a.rows + teams - 1) / teams, NORM_PARTS), per_sm * sm_count());
     return launch_pdl(kernel, dim3(*parts), dim3(threads), smem, st, a);
   };
-  if (cols <= 512) return go(rmsnorm_backward_kernel<2, 1, 4, SKIP>, 256, 4, 8);
-  if (cols <= 1024) return go(rmsnorm_backward_kernel<4, 1, 3, SKIP>, 256, 3, 8);
-  if (cols <= 2048) return go(rmsnorm_backward_kernel<1, 8, 4, SKIP>, 256, 4);
-  if (cols <= 4096) return go(rmsnorm_backward_kernel<1, 16, 4, SKIP>, 512, 4);
-  if (cols <= 8192) return go(rmsnorm_backward_kernel<2, 16, SKIP ? 3 : 4, SKIP>, 512, SKIP ? 3 : 4);   // 8000 of 7168 without dres, three stages 75 us, four 70
-  return go(rmsnorm_backward_kernel<4, 16, 2, SKIP>, 512, 2);   // NORM_COLS
+  // Threads as a row needs them instead of the whole 256 or 512, where that leaves room for another block or a tenth fewer; us, whole / fit: with dres 39893
+  // rows of 1504 97 / 94, 23076 of 2600 106 / 100, 12000 of 5000 110 / 100, 8370 of 7168 88 / 79; without 23076 of 2600 88 / 84, 12000 of 5000 82 / 77.
+  // Where it does not, the count known in advance is better: with dres 16483 of 3640 97 / 100, 14648 of 4096 84 / 88, 5000 of 12000 93 / 96, without
+  // 9146 of 6560 73 / 76.
+  auto fit = [&](int keep) { return ((a.vec_per_row + keep - 1) / keep + 31) & ~31; };
+  if (cols <= 512) return go(rmsnorm_backward_kernel<2, 1, 4, SKIP, false>, 256, 4, 8);
+  if (cols <= 1024) return go(rmsnorm_backward_kernel<4, 1, 3, SKIP, false>, 256, 3, 8);
+  if (cols <= 2048)
+    return fit(1) < 256 ? go(rmsnorm_backward_kernel<1, 8, 4, SKIP, true>, fit(1), 4) : go(rmsnorm_backward_kernel<1, 8, 4, SKIP, false>, 256, 4);
+  if (cols <= 4096)
+    return fit(1) <= 384 ? go(rmsnorm_backward_kernel<1, 16, 4, SKIP, true>, fit(1), 4) : go(rmsnorm_backward_kernel<1, 16, 4, SKIP, false>, 512, 4);
+  if (cols <= 8192)   // without dres four stages leave one block per SM: 7500 of 8000 99 us, 72 so
+    return fit(2) <= (SKIP ? 448 : 384) ? go(rmsnorm_backward_kernel<2, 16, 3, SKIP, true>, fit(2), 3) : go(rmsnorm_backward_kernel<2, 16, 3, SKIP, false>, 512, 3);
+  return go(rmsnorm_backward_kernel<4, 16, 2, SKIP, false>, 512, 2);   // NORM_COLS
 }
 
 }  // namespace
