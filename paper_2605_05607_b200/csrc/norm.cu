@@ -322,17 +322,18 @@ cudaError_t launch_norm(const NormArgs& a, cudaStream_t st) {
   return go(rmsnorm_kernel<8, 8, RES, QUANT>, 256, 1);
 }
 
+constexpr int NORM_SMEM = 226 * 1024;   // an SM's, less what the system and the kernel itself take of a block's 227 KiB
 // Blocks per SM as shared memory, registers and NORM_PARTS (four per SM) allow.
 template <bool SKIP>
 cudaError_t launch_norm_bwd(const NormBwdArgs& a, int* parts, cudaStream_t st) {
   const int cols = a.vec_per_row * VEC;
   auto go = [&](auto kernel, int threads, int stages, int teams = 1) {
     const int smem = teams * stages * (SKIP ? 3 : 2) * cols * 2;
-    if (smem > 40 * 1024) {   // beyond 48 KiB with what the kernel declares itself
-      const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (smem > 40 * 1024) {   // beyond 48 KiB with what the kernel declares itself; always the most, as another thread may be about to launch with more than this
+      const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, NORM_SMEM);
       if (e != cudaSuccess) return e;
     }
-    const int per_sm = max(1, min(min(4, 1152 / threads), 226 * 1024 / (smem + 1280)));
+    const int per_sm = max(1, min(min(4, 1152 / threads), NORM_SMEM / (smem + 1280)));
     *parts = min(min((a.rows + teams - 1) / teams, NORM_PARTS), per_sm * sm_count());
     return launch_pdl(kernel, dim3(*parts), dim3(threads), smem, st, a);
   };

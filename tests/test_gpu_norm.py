@@ -229,3 +229,33 @@ def test_norm_captured_and_on_another_stream():
     for got, name in ((y, "y"), (q, "q"), (sc, "scale"), (rs, "rstd"), (res, "res")):
         assert torch.equal(got, want[name]), name
     assert torch.equal(dx, bwd[0]) and torch.equal(dw, bwd[1])
+
+
+def test_norm_backward_by_two_threads_at_once():
+    """Widths that share a kernel and differ in its shared memory: neither thread takes from the other what its launch needs."""
+    import threading
+    jobs, errors = [], []
+    for cols in (4104, 8192, 6000):
+        x, r, w = make(40, cols, cols)
+        out, dy, k = forward(x, r, w, q=False), torch.randn_like(x), torch.randn_like(x)
+        jobs.append((cols, out, w, dy, k, backward(dy, out["res"], w, out["rstd"], k), torch.empty_like(x),
+                     torch.empty(cols, device="cuda"),
+                     torch.empty(B.moe_rmsnorm_backward_workspace_bytes(40, cols), dtype=torch.uint8, device="cuda"),
+                     torch.cuda.Stream()))
+    torch.cuda.synchronize()
+
+    def run(cols, out, w, dy, k, want, dx, dw, ws, stream):
+        try:
+            for _ in range(400):
+                B.moe_rmsnorm_backward(dy, out["res"], w, out["rstd"], dx, dw, ws, dres=k, stream=stream)
+            stream.synchronize()
+            assert torch.equal(dx, want[0]) and torch.equal(dw, want[1])
+        except Exception as e:   # noqa: BLE001
+            errors.append((cols, e))
+
+    threads = [threading.Thread(target=run, args=j) for j in jobs]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors, errors
