@@ -445,8 +445,8 @@ long long fp4_row_sets(const Shape& s) {
 // 97 / 117, 3000, top-2 of 64 x 2048 x 2048 (94) 108 / 120, 3200, top-4 of 128 x 2048 x 1024 (100) 133 / 133, 3318 on 32 x 1888 x 7168 (104) 217 / 198, 1777
 // skewed, top-4 of 64 x 2880 x 2880 (111) 225 / 252, 450, top-2 of 8 x 4096 x 4096 (112) 66 / 66, 1000 skewed, top-4 of 32 x 1024 x 1024 (125) 37 / 41,
 // 4096, top-2 of 64 x 2048 x 2048 (128) 135 / 128, 2900, top-2 of 32 x 2880 x 2880 (181) 156 / 135, 800, top-2 of 8 x 2048 x 7168 (200) 77 / 67, 3600
-// skewed on 16 x 4096 x 1536 (225) 81 / 79.  (Both forms side by side, each for the experts of its kind, gained nothing where
-// routing is skewed and lost where tiles are few.)
+// skewed on 16 x 4096 x 1536 (225) 81 / 79.  Near the rule the routing decides: 1900, top-8 of 128 x 4096 x 1536 (119) even 349 / 318, skewed 328 / 364.
+// (Both forms side by side, each for the experts of its kind, gained nothing where routing is skewed and lost where tiles are few.)
 static bool fp4_pairs(const Shape& s) { return (long long)s.T * s.k >= 128ll * s.E; }
 
 // Whether a product's tiles (at most row_tiles * ceil(N / width)) are shared.  A CTA streams at most 63 KB/us, all together 6.5 TB/s: tiles that leave SMs
