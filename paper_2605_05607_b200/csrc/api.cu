@@ -20,6 +20,7 @@ inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 struct WsPlan {
   size_t status, emask, gmask, eprefix, gprefix, mt_prefix, mp_prefix, blk_start, blk_info, n_blocks, tracker, wsplit, xs, h, hq, sh, xq, sx, o, logits, topk_idx, topk_w;
   size_t expert_counts, expert_offsets, group_counts, group_offsets, pair_row, row_pair, al, disp_token, row_src, sf_x, sf_h, part4, arrived4;
+  size_t base;    // end of the regions of every form but FP4
   size_t total;
   int W;
 };
@@ -90,7 +91,8 @@ WsPlan plan(const moe_shape_t& s) {
   p.al = take(G * T * 4);
   p.disp_token = take(T * kg * 4);
   p.row_src = take(P * 4);
-  // FP4 form: scale chunks of the row tiles of x and of h (the sorted codes of x lie in `o`, those of h in `h`)
+  p.base = off;
+  // FP4 form, behind what the others use: scale chunks of the row tiles of x and of h (the sorted codes of x lie in `o`, those of h in `h`)
   const bool fp4 = s.d % 32 == 0 && s.f % 32 == 0;
   p.sf_x = take(fp4 ? fp4_scale_bytes((size_t)fp4_row_sets(to_shape(s)), s.d) : 0);
   p.sf_h = take(fp4 ? fp4_scale_bytes((size_t)fp4_row_sets(to_shape(s)), s.f) : 0);
@@ -123,11 +125,12 @@ int check_shape(const moe_shape_t* s) {
 
 inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
-int check_ws(const moe_shape_t* s, const void* ws, size_t ws_bytes, WsPlan* out) {
+// A call asks for the regions of its own form only: one that needs none of the FP4 form's takes a workspace without them.
+int check_ws(const moe_shape_t* s, const void* ws, size_t ws_bytes, WsPlan* out, bool fp4 = false) {
   if (ws == nullptr) return MOE_ERR_INVALID_ARG;
   if (!aligned(ws, 128)) return MOE_ERR_MISALIGNED;
   *out = plan(*s);
-  if (ws_bytes < out->total) return MOE_ERR_WORKSPACE_TOO_SMALL;
+  if (ws_bytes < (fp4 ? out->total : out->base)) return MOE_ERR_WORKSPACE_TOO_SMALL;
   return MOE_OK;
 }
 
@@ -828,7 +831,7 @@ int moe_expert_ffn_fp4(const moe_shape_t* shape, const void* xq, const void* sx,
   if ((rc = check_layout(layout)) != MOE_OK) return rc;
   if (!aligned(xq, 128) || !aligned(o, 128) || !aligned(topk_w, 16)) return MOE_ERR_MISALIGNED;
   WsPlan p;
-  if ((rc = check_ws(shape, ws, ws_bytes, &p)) != MOE_OK) return rc;
+  if ((rc = check_ws(shape, ws, ws_bytes, &p, true)) != MOE_OK) return rc;
   if (!have_device()) return MOE_ERR_CUDA;
   FfnArgs a{};
   a.a_src = xq;
@@ -893,7 +896,7 @@ static int layer_impl(const moe_shape_t* shape, const void* x, const float* w_ga
       !aligned(logit_bias, 4))
     return MOE_ERR_MISALIGNED;
   WsPlan p;
-  if ((rc = check_ws(shape, ws, ws_bytes, &p)) != MOE_OK) return rc;
+  if ((rc = check_ws(shape, ws, ws_bytes, &p, fp4 != nullptr)) != MOE_OK) return rc;
   if (!have_device()) return MOE_ERR_CUDA;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const Shape s = to_shape(*shape);

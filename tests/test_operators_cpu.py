@@ -185,3 +185,39 @@ def test_norm_oracle_against_differences():
         d = np.zeros_like(w)
         d[j] = h
         assert abs((c * (N.rmsnorm(x, r, w + d, 0.1)[2] - N.rmsnorm(x, r, w - d, 0.1)[2])).sum() / (2 * h) - dw[j]) < 1e-7
+
+
+# ---- workspaces -------------------------------------------------------------------------------------------------------------
+def workspace_calls(L, sh, n):
+    """Return codes of the entry points that take a workspace, given n bytes of it: those of the bf16 and E4M3 forms, then the FP4 ones."""
+    r, lay = ctypes.byref(sh), ctypes.byref(layout())
+    others = {
+        "moe_route": L.moe_route(r, P, P, None, 0, P, P, P, P, n, None),
+        "moe_dispatch": L.moe_dispatch(r, P, P, lay, P, P, n, None),
+        "moe_expert_ffn": L.moe_expert_ffn(r, P, lay, P, P, P, P, P, P, n, None),
+        "moe_expert_ffn_fp8": L.moe_expert_ffn_fp8(r, P, P, lay, P, P, P, P, P, P, P, P, P, n, None),
+        "moe_combine": L.moe_combine(r, P, lay, P, P, None, P, P, n, None),
+        "moe_layer": L.moe_layer(r, P, P, None, 0, P, P, P, P, None, None, None, None, P, n, None),
+        "moe_layer_fp8": L.moe_layer_fp8(r, P, P, None, 0, P, P, P, P, P, P, P, None, None, None, None, P, n, None),
+    }
+    fp4 = {
+        "moe_expert_ffn_fp4": L.moe_expert_ffn_fp4(r, P, P, lay, P, P, P, P, P, P, P, P, P, n, None),
+        "moe_layer_fp4": L.moe_layer_fp4(r, P, P, None, 0, P, P, P, P, P, P, P, None, None, None, None, P, n, None),
+    }
+    return others, fp4
+
+
+# what the bf16 and E4M3 forms use, the sum of their regions
+@pytest.mark.skipif(not NO_GPU, reason="the calls are accepted, and stop where they find no device")
+@pytest.mark.parametrize("dims,own", [((1, 4096, 14336, 8, 2, 2), 131072), ((4, 2048, 7168, 16, 2, 1), 238592), ((3, 4096, 4096, 8, 1, 1), 122880),
+                                      ((100, 288, 160, 4, 2, 2), 268288), ((2048, 64, 96, 4, 2, 2), 2055168)], ids=str)
+def test_only_the_fp4_form_asks_for_its_regions(L, dims, own):
+    sh = shape(**dict(zip(("T", "d", "f", "E", "k", "G"), dims)))
+    most = B.moe_workspace_bytes(sh)
+    assert most > own
+    others, fp4 = workspace_calls(L, sh, own)
+    assert set(others.values()) == {CUDA} and set(fp4.values()) == {SMALL}, (others, fp4)
+    others, _ = workspace_calls(L, sh, own - 1)
+    assert set(others.values()) == {SMALL}, others
+    others, fp4 = workspace_calls(L, sh, most)
+    assert set(others.values()) | set(fp4.values()) == {CUDA}, (others, fp4)
