@@ -141,8 +141,8 @@ typedef struct {
   int32_t* row_src;         /* [T*k]  dispatched row feeding expert row r                */
 } moe_layout_t;
 
-/* Bytes of workspace that any entry point may need for this shape.  (Only the FP4 entry points ask for all of them: the others take a workspace that
- * lacks what the FP4 form alone uses.) */
+/* Bytes of workspace that any entry point may need for this shape, or for one of fewer tokens that is the same otherwise.  (Only the
+ * FP4 entry points ask for all of them: the others take a workspace that lacks what the FP4 form alone uses.) */
 int moe_workspace_bytes(const moe_shape_t* shape, size_t* bytes);
 
 /* Zero the status block of a workspace (enqueued on `stream`). */

@@ -20,7 +20,6 @@ inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 struct WsPlan {
   size_t status, emask, gmask, eprefix, gprefix, mt_prefix, mp_prefix, blk_start, blk_info, n_blocks, tracker, wsplit, xs, h, hq, sh, xq, sx, o, logits, topk_idx, topk_w;
   size_t expert_counts, expert_offsets, group_counts, group_offsets, pair_row, row_pair, al, disp_token, row_src, sf_x, sf_h, part4, arrived4;
-  size_t base;    // end of the regions of every form but FP4
   size_t total;
   int W;
 };
@@ -40,7 +39,9 @@ bool pair_gemm1(const moe_shape_t& s) {
 
 Shape to_shape(const moe_shape_t& s) { return Shape{s.T, s.d, s.f, s.E, s.k, s.G, s.score_fn, s.flags}; }
 
-WsPlan plan(const moe_shape_t& s) {
+// No region is smaller for more tokens (all else the same): a workspace for the largest batch serves every smaller one.
+// fp4: with the regions that the FP4 form alone uses, behind the others.
+WsPlan plan(const moe_shape_t& s, bool fp4) {
   WsPlan p{};
   const size_t T = (size_t)s.T, E = (size_t)s.E, G = (size_t)s.G, k = (size_t)s.k;
   const size_t P = T * k;
@@ -91,9 +92,8 @@ WsPlan plan(const moe_shape_t& s) {
   p.al = take(G * T * 4);
   p.disp_token = take(T * kg * 4);
   p.row_src = take(P * 4);
-  p.base = off;
-  // FP4 form, behind what the others use: scale chunks of the row tiles of x and of h (the sorted codes of x lie in `o`, those of h in `h`)
-  const bool fp4 = s.d % 32 == 0 && s.f % 32 == 0;
+  // FP4 form: scale chunks of the row tiles of x and of h (the sorted codes of x lie in `o`, those of h in `h`)
+  fp4 = fp4 && s.d % 32 == 0 && s.f % 32 == 0;
   p.sf_x = take(fp4 ? fp4_scale_bytes((size_t)fp4_row_sets(to_shape(s)), s.d) : 0);
   p.sf_h = take(fp4 ? fp4_scale_bytes((size_t)fp4_row_sets(to_shape(s)), s.f) : 0);
   p.part4 = take(fp4 ? fp4_part_bytes(to_shape(s)) : 0);
@@ -129,8 +129,8 @@ inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_
 int check_ws(const moe_shape_t* s, const void* ws, size_t ws_bytes, WsPlan* out, bool fp4 = false) {
   if (ws == nullptr) return MOE_ERR_INVALID_ARG;
   if (!aligned(ws, 128)) return MOE_ERR_MISALIGNED;
-  *out = plan(*s);
-  if (ws_bytes < (fp4 ? out->total : out->base)) return MOE_ERR_WORKSPACE_TOO_SMALL;
+  *out = plan(*s, fp4);
+  if (ws_bytes < out->total) return MOE_ERR_WORKSPACE_TOO_SMALL;
   return MOE_OK;
 }
 
@@ -356,7 +356,7 @@ int moe_workspace_bytes(const moe_shape_t* shape, size_t* bytes) {
   int rc = check_shape(shape);
   if (rc != MOE_OK) return rc;
   if (bytes == nullptr) return MOE_ERR_INVALID_ARG;
-  *bytes = plan(*shape).total;
+  *bytes = plan(*shape, true).total;
   return MOE_OK;
 }
 
@@ -364,7 +364,7 @@ int moe_workspace_layout(const moe_shape_t* shape, size_t out[4]) {
   int rc = check_shape(shape);
   if (rc != MOE_OK) return rc;
   if (out == nullptr) return MOE_ERR_INVALID_ARG;
-  const WsPlan p = plan(*shape);
+  const WsPlan p = plan(*shape, true);
   out[0] = p.status;
   out[1] = p.h;
   out[2] = p.o;

@@ -462,10 +462,29 @@ static int fp4_part_rows(const Shape& s) {
   const long long P = (long long)s.T * s.k;
   return P < ffn::F4_ROWS ? (int)(P + 15) & ~15 : ffn::F4_ROWS;
 }
-size_t fp4_part_bytes(const Shape& s) {
-  return fp4_share1(s) || fp4_share2(s) ? (size_t)2 * ffn::F4_CTAS * fp4_part_rows(s) * 256 * 4 : 0;
+static bool fp4_shares(const Shape& s) { return fp4_share1(s) || fp4_share2(s); }
+// Rows that parts are reserved for: those of the largest batch of at most s.T tokens that shares tiles (0 if none does), so that a workspace for many
+// tokens serves fewer.  Tiles only grow with the tokens, so batches share up to some number of tokens, and F4_ROWS rows are the most.
+static int fp4_reserved_rows(const Shape& s) {
+  Shape b = s;
+  b.T = min(s.T, (ffn::F4_ROWS + s.k - 1) / s.k);
+  if (b.T > 0 && !fp4_shares(b)) {
+    int hi = b.T;   // does not share
+    b.T = 1;
+    if (!fp4_shares(b)) b.T = 0;
+    while (hi - b.T > 1 && b.T > 0) {
+      const int low = b.T;
+      b.T = (low + hi) / 2;
+      if (!fp4_shares(b)) {
+        hi = b.T;
+        b.T = low;
+      }
+    }
+  }
+  return b.T > 0 ? fp4_part_rows(b) : 0;
 }
-size_t fp4_arrived_bytes(const Shape& s) { return fp4_share1(s) || fp4_share2(s) ? (size_t)2 * ffn::F4_CTAS * 8 * 4 : 0; }
+size_t fp4_part_bytes(const Shape& s) { return (size_t)2 * ffn::F4_CTAS * fp4_reserved_rows(s) * 256 * 4; }
+size_t fp4_arrived_bytes(const Shape& s) { return fp4_reserved_rows(s) > 0 ? (size_t)2 * ffn::F4_CTAS * 8 * 4 : 0; }
 
 cudaError_t launch_expert_ffn_fp4(const Shape& s, const FfnArgs& a, const Fp4Args& q, cudaStream_t st) {
   if (s.T == 0) return cudaSuccess;
@@ -477,7 +496,7 @@ cudaError_t launch_expert_ffn_fp4(const Shape& s, const FfnArgs& a, const Fp4Arg
   const int chunk = P >= 8 * 64 * sm_count() ? 4 : 1;
   cudaError_t e = launch_pdl(ffn::fp4_sort_kernel, dim3((unsigned)((P + 8 * chunk - 1) / (8 * chunk))), dim3(256), 0, st, static_cast<const uint4*>(a.a_src),
                              q.sx, a.a_rows, a.gather_idx, a.gather_div, a.expert_offsets, s.E, s.d, P, rows1, chunk, static_cast<uint4*>(a.xs), q.sfx,
-                             a.topk_w, a.row_pair, row_w, q.arrived, (int)(fp4_arrived_bytes(s) / 4), a.status);
+                             a.topk_w, a.row_pair, row_w, q.arrived, fp4_shares(s) ? 2 * ffn::F4_CTAS * 8 : 0, a.status);
   if (e != cudaSuccess) return e;
   ffn::F4Params g1{};
   g1.expert_offsets = a.expert_offsets;

@@ -221,3 +221,13 @@ def test_only_the_fp4_form_asks_for_its_regions(L, dims, own):
     assert set(others.values()) == {SMALL}, others
     others, fp4 = workspace_calls(L, sh, most)
     assert set(others.values()) | set(fp4.values()) == {CUDA}, (others, fp4)
+
+
+@pytest.mark.parametrize("E,k,G", [(1, 1, 1), (8, 2, 2), (8, 1, 1), (16, 2, 1), (64, 6, 8), (128, 8, 8)], ids=str)
+@pytest.mark.parametrize("d,f", [(64, 2048), (2048, 7168), (4096, 4096), (4096, 14336), (7168, 2048), (512, 4096)], ids=str)
+def test_workspace_of_a_batch_serves_smaller_ones(L, d, f, E, k, G):
+    prev = 0
+    for T in [*range(0, 300), 511, 512, 1000, 2047, 2048, 4096, 16384, 65536]:
+        now = B.moe_workspace_bytes(shape(T=T, d=d, f=f, E=E, k=k, G=G))
+        assert now >= prev, (T, prev, now)
+        prev = now
