@@ -369,7 +369,12 @@ __global__ void __launch_bounds__(256) fp4_sort_kernel(const uint4* __restrict__
       report_error(status, DEV_INDEX_OUT_OF_RANGE, KID_GEMM1, src, r);
       src = -1;
     }
-    if (row_w != nullptr) row_w[r] = __ldg(topk_w + __ldg(row_pair + r));
+    if (row_w != nullptr) {   // nothing is read with a number that lies outside the batch
+      const int pair = __ldg(row_pair + r);
+      const bool valid = pair >= 0 && pair < capacity;
+      if (!valid) report_error(status, DEV_INDEX_OUT_OF_RANGE, KID_GEMM1, pair, r);
+      row_w[r] = valid ? __ldg(topk_w + pair) : 0.f;
+    }
   }
   for (int j = 0; j < n; ++j) {
     const int s = __shfl_sync(0xFFFFFFFFu, src, j);

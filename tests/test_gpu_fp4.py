@@ -428,3 +428,18 @@ def test_norm_stays_inside_its_buffers(rows, cols):
     B.moe_rmsnorm_backward(dy, s, w, rs, dx, dw, buf(B.moe_rmsnorm_backward_workspace_bytes(rows, cols), fill=0xEE), dres=r)
     buf.check()
     assert torch.isfinite(dx.float()).all() and torch.isfinite(dw).all()
+
+
+@pytest.mark.parametrize("row,pair", [(4, 1 << 30), (4, 30), (7, -1), (29, -(1 << 31))])
+def test_expert_ffn_fp4_reports_a_pair_out_of_range(row, pair):
+    """The gate weight is not read with a pair that is not in the batch; the other rows are those of a sound layout."""
+    shape, ws, lay, x, xg, idx, w, wt = routed((10, 20), d=64, f=64, seed=1)
+    q, rows = quantised(wt), rows_fp4(xg)
+    want, o = (torch.zeros(30, 64, device="cuda").bfloat16() for _ in range(2))
+    B.moe_expert_ffn_fp4(shape, *rows, lay, w, *q, want, ws)
+    lay.row_pair[row] = pair
+    B.moe_expert_ffn_fp4(shape, *rows, lay, w, *q, o, ws)
+    st = B.moe_status(ws)
+    assert st[0] == B.MOE_DEV_INDEX_OUT_OF_RANGE and st[2] == pair and st[3] == row
+    keep = torch.arange(30, device="cuda") != row
+    assert torch.equal(o[keep], want[keep])
