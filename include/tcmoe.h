@@ -310,8 +310,9 @@ int moe_layer_fp8_host(const moe_shape_t* shape, const void* x_host, void* x_dev
  *   x, residual [rows, cols] bf16 (residual may be NULL: s = x);  weight [cols] bf16, or fp32 with weight_f32 != 0
  *   res_out     NULL, or bf16 out: s (needs residual);  y NULL, or bf16 out;  yq, scale both NULL, or E4M3 codes [rows, cols] and fp32 [rows]
  *   rstd        NULL, or fp32 [rows] out, for moe_rmsnorm_backward.  At least one of y and yq is not NULL.
- * res_out and y may be x or residual themselves (not both the same buffer).  A row that holds a NaN or an infinity gives NaN; eps = 0 gives
- * NaN for a row of zeros.  Limits: cols % 8 == 0, cols <= 16384 (MOE_ERR_UNSUPPORTED_SHAPE); eps >= 0.  Alignment: 16 bytes, yq 8, scale
+ * res_out and y may be x or residual themselves (not both the same buffer).  The mean is taken in fp32: a row where it is not finite
+ * (a NaN, an infinity, or values of about 1e19 and more, whose squares are not) gives NaN throughout, rstd, scale and codes included (res_out is s
+ * all the same); so does, with eps = 0, a row whose mean vanishes.  Limits: cols % 8 == 0, cols <= 16384 (MOE_ERR_UNSUPPORTED_SHAPE); eps >= 0.  Alignment: 16 bytes, yq 8, scale
  * and rstd 4.  rows = 0 is accepted.  No workspace. */
 int moe_rmsnorm(const void* x, const void* residual, const void* weight, int32_t weight_f32, float eps, int64_t rows, int64_t cols,
                 void* res_out, void* y, void* yq, float* scale, float* rstd, void* stream);
@@ -320,6 +321,7 @@ int moe_rmsnorm(const void* x, const void* residual, const void* weight, int32_t
  * weight and xhat = s * rstd:
  *     dx = rstd * (g - xhat * mean(g * xhat)) + dres          bf16 [rows, cols]: the gradient of x and of residual alike
  *     dweight = sum over the rows of dy * xhat                fp32 [cols], written whole (zeros for rows = 0)
+ * A row whose rstd is NaN makes its dx and all of dweight NaN.
  * dres (NULL, or bf16 [rows, cols]) is the gradient that reaches s past the norm, through the skip path.  dx may be dy, dres or s.
  * fp32 arithmetic, no atomics: the same bits every time.  ws: moe_rmsnorm_backward_workspace_bytes(rows, cols) bytes, 16-byte aligned, used
  * during the call only (it need not be zeroed and has no status block).  Limits and alignment as moe_rmsnorm, rows < 2^31. */

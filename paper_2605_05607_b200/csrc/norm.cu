@@ -1,7 +1,7 @@
 // Root-mean-square norm of the residual stream, the step in front of the layer, with the residual's addition, an E4M3 output with one
 // scale per row (the operand of the FP8 experts), and its backward pass.
 //     s = x + residual                    fp32; leaves as bf16 (the residual stream of the next block)
-//     rstd = 1 / sqrt(mean(s^2) + eps)
+//     rstd = 1 / sqrt(mean(s^2) + eps)     NaN, and with it the row, where the mean is not finite
 //     y = (s * w) * rstd                  leaves as bf16 and / or as codes of y / scale, scale = max|y| / 448
 // Everything is computed from the fp32 sum: y and the codes are rounded once each, from fp32 (codes of the rounded y would round twice).
 // The product with w comes first so that one pass has both sums of the row: rounding is monotone, so max|y| is (max|s * w|) * rstd to the bit.
@@ -104,7 +104,9 @@ __global__ void __launch_bounds__(WARPS == 1 ? 256 : WARPS * 32) rmsnorm_kernel(
       }
       flip ^= 1;
     }
-    const float rstd = __frsqrt_rn(__fadd_rn(__fdiv_rn(sum, (float)(a.vec_per_row * VEC)), a.eps));
+    // A sum that is not finite would give 0, and a row of zeros that look like a result; with eps = 0, squares that vanish an infinity.  NaN both.
+    const float var = __fadd_rn(__fdiv_rn(sum, (float)(a.vec_per_row * VEC)), a.eps);
+    const float rstd = var > 0.f && var <= 3.402823466e38f ? __frsqrt_rn(var) : __uint_as_float(0x7FC00000u);
     if (lane == 0 && a.rstd != nullptr) a.rstd[r] = rstd;
     float sc = 1.f, inv = 1.f;
     bool exact = true;

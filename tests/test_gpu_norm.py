@@ -259,3 +259,46 @@ def test_norm_backward_by_two_threads_at_once():
     for t in threads:
         t.join()
     assert not errors, errors
+
+
+@pytest.mark.parametrize("cols", [512, 1024, 2048, 4096, 8192, 16384])
+@pytest.mark.parametrize("res", [False, True])
+def test_norm_rows_whose_sum_of_squares_is_not_finite(cols, res):
+    """NaN throughout, not zeros that look like a result: a NaN, an infinity, values whose squares or whose sum of squares leave fp32, and a sum with the
+    residual that does.  The rows beside them are those of a call without them."""
+    x, r, w = make(9, cols, cols, res)
+    want = forward(x, r, w)
+    bad = torch.tensor([1, 2, 3, 4, 6, 7], device="cuda")
+    x[1, 3], x[2, cols - 1], x[3, 0] = float("nan"), float("inf"), -float("inf")
+    x[4, 5] = 2e19                               # its square is not finite
+    x[6] = 1.8e19                                # each square is, their sum is not
+    if res:
+        x[7], r[7] = 3e38, 3e38
+    else:
+        x[7] = -3.3e38
+    out = forward(x, r, w)
+    good = torch.tensor([0, 5, 8], device="cuda")
+    for name, t in out.items():
+        assert torch.equal(t[good], want[name][good]), name
+    assert torch.isnan(out["y"][bad]).all() and torch.isnan(out["rstd"][bad]).all() and torch.isnan(out["scale"][bad]).all()
+    assert np.isnan(e4m3(out["q"][bad])).all()
+    if res:
+        assert torch.equal(torch.nan_to_num(out["res"], 7.0), torch.nan_to_num((x.float() + r.float()).bfloat16(), 7.0))
+    # the backward passes the NaN on, to its own rows of dx and to dw
+    g = torch.Generator(device="cuda").manual_seed(1)
+    dy = torch.randn(9, cols, generator=g, device="cuda").bfloat16()
+    s = out["res"] if res else x
+    dx, dw = backward(dy, s, w, out["rstd"])
+    assert torch.isnan(dx[bad]).all() and torch.isfinite(dx[good]).all() and torch.isnan(dw).all()
+
+
+def test_norm_of_large_values_within_range():
+    """Squares near the end of fp32, and at its beginning with eps = 0."""
+    for cols in (64, 4096, 16384):
+        x, r, w = make(40, cols, 2, True, True)
+        top = 1.8e19 / (5 * cols) ** 0.5 / 4     # cols squares of about 0.6 top^2 are 2.5e36
+        x, r = (x.float() * top / 4).bfloat16(), (r.float() * top / 4).bfloat16()
+        check_forward(x, r, w, forward(x, r, w))
+    # eps = 0 and squares that vanish: NaN, as for a row of zeros
+    tiny = forward(torch.full((1, 256), 1e-25, device="cuda").bfloat16(), None, torch.ones(256, device="cuda"), eps=0.0)
+    assert torch.isnan(tiny["y"]).all() and torch.isnan(tiny["scale"]).all() and torch.isnan(tiny["rstd"]).all()
