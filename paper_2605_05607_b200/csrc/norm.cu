@@ -146,7 +146,8 @@ struct NormBwdArgs {
   const void* w;
   int w32;
   const float* rstd;
-  int rows, vec_per_row;
+  long long rows;
+  int vec_per_row;
   uint4* dx;
   float* part;            // [grid, columns]
 };
@@ -324,6 +325,13 @@ cudaError_t launch_norm(const NormArgs& a, cudaStream_t st) {
   return go(rmsnorm_kernel<8, 8, RES, QUANT>, 256, 1);
 }
 
+// Blocks of the backward pass: `teams` rows at a time each, no more than there is room for.
+constexpr int rmsnorm_blocks(long long rows, int teams, int resident) {
+  const long long blocks = (rows + teams - 1) / teams, most = resident < NORM_PARTS ? resident : NORM_PARTS;
+  return (int)(blocks < most ? blocks : most);
+}
+static_assert(rmsnorm_blocks((1ll << 31) - 1, 8, 592) == 592 && rmsnorm_blocks(9, 8, 592) == 2, "up to the largest row count");
+
 constexpr int NORM_SMEM = 226 * 1024;   // an SM's, less what the system and the kernel itself take of a block's 227 KiB
 // Blocks per SM as shared memory, registers and NORM_PARTS (four per SM) allow.
 template <bool SKIP>
@@ -336,7 +344,7 @@ cudaError_t launch_norm_bwd(const NormBwdArgs& a, int* parts, cudaStream_t st) {
       if (e != cudaSuccess) return e;
     }
     const int per_sm = max(1, min(min(4, 1152 / threads), NORM_SMEM / (smem + 1280)));
-    *parts = min(min((a.rows + teams - 1) / teams, NORM_PARTS), per_sm * sm_count());
+    *parts = rmsnorm_blocks(a.rows, teams, per_sm * sm_count());
     return launch_pdl(kernel, dim3(*parts), dim3(threads), smem, st, a);
   };
   // Threads as a row needs them instead of the whole 256 or 512, where that leaves room for another block or a tenth fewer; us, whole / fit: with dres 39893
@@ -373,7 +381,7 @@ cudaError_t launch_rmsnorm_backward(const void* dy, const void* dres, const void
   int parts = 0;
   if (rows > 0) {
     const NormBwdArgs a{static_cast<const uint4*>(dy), static_cast<const uint4*>(dres), static_cast<const uint4*>(s), w, w32 ? 1 : 0, rstd,
-                        (int)rows, cols / VEC, static_cast<uint4*>(dx), part};
+                        rows, cols / VEC, static_cast<uint4*>(dx), part};
     const cudaError_t e = dres != nullptr ? launch_norm_bwd<true>(a, &parts, st) : launch_norm_bwd<false>(a, &parts, st);
     if (e != cudaSuccess) return e;
   }

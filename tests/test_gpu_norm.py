@@ -302,3 +302,30 @@ def test_norm_of_large_values_within_range():
     # eps = 0 and squares that vanish: NaN, as for a row of zeros
     tiny = forward(torch.full((1, 256), 1e-25, device="cuda").bfloat16(), None, torch.ones(256, device="cuda"), eps=0.0)
     assert torch.isnan(tiny["y"]).all() and torch.isnan(tiny["scale"]).all() and torch.isnan(tiny["rstd"]).all()
+
+
+def test_norm_backward_of_the_most_rows():
+    """2^31 - 1 rows, the limit: row numbers and the rounding up to whole blocks need more than 32 bits.  Rows of 8 columns, dx over dy."""
+    rows, cols = (1 << 31) - 1, 8
+    if torch.cuda.mem_get_info()[0] < 100e9:
+        pytest.skip("needs 86 GB of device memory")
+    s = torch.ones(rows, cols, dtype=torch.bfloat16, device="cuda")
+    dy = torch.zeros(rows, cols, dtype=torch.bfloat16, device="cuda")
+    rstd = torch.full((rows,), 0.5, device="cuda")
+    hot = [0, 7, 4735, 1 << 30, rows - 9, rows - 8, rows - 1]
+    for i in hot:
+        dy[i, 3] = 2.0
+    w, dw = torch.ones(cols, device="cuda"), torch.full((cols,), 7.0, device="cuda")
+    ws = torch.empty(B.moe_rmsnorm_backward_workspace_bytes(rows, cols), dtype=torch.uint8, device="cuda")
+    B.moe_rmsnorm_backward(dy, s, w, rstd, dy, dw, ws)
+    torch.cuda.synchronize()
+    # g = 2 e_3, xhat = 0.5: dx = 0.5 (g - 0.5 * mean(g * 0.5)) = e_3 - 0.03125; dw_3 = 2 * 0.5 per row
+    want = torch.full((cols,), -0.03125)
+    want[3] += 1
+    for i in hot:
+        assert torch.equal(dy[i].float().cpu(), want), i
+        dy[i] = 0
+    assert dw.tolist() == [0, 0, 0, len(hot), 0, 0, 0, 0]
+    assert not any(part.any().item() for part in dy.split(1 << 27))
+    del s, dy, rstd
+    torch.cuda.empty_cache()
