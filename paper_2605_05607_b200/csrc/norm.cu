@@ -321,8 +321,8 @@ cudaError_t launch_norm(const NormArgs& a, cudaStream_t st) {
   if (cols <= 4096) return go(rmsnorm_kernel<4, 4, RES, QUANT>, 128, 1);
   if (cols <= 8192) return go(rmsnorm_kernel<4, 8, RES, QUANT>, 256, 1);
   // to NORM_COLS; us with 256 / 512 threads per row: 4187 rows of 16000, bf16 alone, 53.5 / 79.4, with residual and both outputs (spilled) 160 / 115
-  if (RES) return go(rmsnorm_kernel<4, 16, RES, QUANT>, 512, 1);
-  return go(rmsnorm_kernel<8, 8, RES, QUANT>, 256, 1);
+  if constexpr (RES) return go(rmsnorm_kernel<4, 16, RES, QUANT>, 512, 1);
+  else return go(rmsnorm_kernel<8, 8, RES, QUANT>, 256, 1);
 }
 
 // Blocks of the backward pass: `teams` rows at a time each, no more than there is room for.
