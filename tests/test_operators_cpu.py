@@ -231,3 +231,19 @@ def test_workspace_of_a_batch_serves_smaller_ones(L, d, f, E, k, G):
         now = B.moe_workspace_bytes(shape(T=T, d=d, f=f, E=E, k=k, G=G))
         assert now >= prev, (T, prev, now)
         prev = now
+
+
+@pytest.mark.parametrize("has_lookup", [True, False])
+def test_current_stream_with_and_without_the_direct_lookup(monkeypatch, has_lookup):
+    """Which the calls get without a stream: the current one of the current device, also from a torch that lacks the lookup that is not public."""
+    class Fake:
+        cuda_stream = 4321
+    monkeypatch.setattr(B, "_have_cuda", True)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 3)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda: Fake)
+    if has_lookup:
+        monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 1000 + device, raising=False)
+    else:
+        monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream", raising=False)
+    assert B._stream(None) == (1003 if has_lookup else 4321)
+    assert B._stream(Fake) == 4321
