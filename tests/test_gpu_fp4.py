@@ -443,3 +443,109 @@ def test_expert_ffn_fp4_reports_a_pair_out_of_range(row, pair):
     assert st[0] == B.MOE_DEV_INDEX_OUT_OF_RANGE and st[2] == pair and st[3] == row
     keep = torch.arange(30, device="cuda") != row
     assert torch.equal(o[keep], want[keep])
+
+
+# ---- sizes at which the kernels' loops come round again --------------------------------------------------------------------------
+def test_rows_fp4_beyond_one_pass_of_the_grid():
+    """The grid takes 16 blocks per SM x 8192 values at once (19.4 M on 148 SMs): 2.1 times as many, against calls of 1000 rows, which one pass takes."""
+    cols = 2880
+    rows = int(2.1 * 16 * torch.cuda.get_device_properties(0).multi_processor_count * 8192) // cols + 1
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn(rows, cols, generator=g, device="cuda").mul_(torch.exp2(8 * torch.rand(rows, 1, generator=g, device="cuda"))).bfloat16()
+    q, s = rows_fp4(x)
+    back = torch.full_like(x, 7.0)
+    B.moe_dequantize_rows_fp4(q, s, back)
+    for i in range(0, rows, 1000):
+        qi, si = rows_fp4(x[i:i + 1000])
+        bi = torch.full_like(x[i:i + 1000], 7.0)
+        B.moe_dequantize_rows_fp4(qi, si, bi)
+        assert torch.equal(q[i:i + 1000], qi) and torch.equal(s[i:i + 1000], si) and torch.equal(back[i:i + 1000], bi), i
+    q_ref, s_ref = Q.quantize_rows(f64(x[-300:]))
+    assert np.array_equal(q[-300:].cpu().numpy(), q_ref) and np.array_equal(s[-300:].cpu().numpy(), s_ref)
+
+
+def with_empty_experts(T, E, k, d, f, flags=0, seed=0):
+    """T tokens over E experts, of which every fifth and the first and last two get none; the others' rows fall off from expert to expert."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    score = torch.rand(T, E, generator=g, device="cuda") - 0.6 * torch.arange(E, device="cuda") / E
+    score[:, ::5] = score[:, :2] = score[:, -2:] = -9
+    idx = score.topk(k, dim=1).indices.int()
+    if flags & B.MOE_FLAG_SPARSE_TOPK:
+        idx[torch.rand(T, k, generator=g, device="cuda") < 0.03] = -1
+    shape = B.MoEShape(T, d, f, E, k, 1, 0, flags)
+    ws, lay = B.alloc_workspace(shape), B.alloc_layout(shape)
+    x = torch.randn(T, d, generator=g, device="cuda").mul_(torch.exp2(4 * torch.rand(T, 1, generator=g, device="cuda"))).bfloat16()
+    B.moe_dispatch(shape, None, idx.contiguous(), lay, None, ws)
+    w = torch.rand(T, k, generator=g, device="cuda") + 0.1
+    wt = [torch.randn(E, K, N, generator=g, device="cuda").div(K ** 0.5).bfloat16() for K, N in ((d, f), (d, f), (f, d))]
+    return shape, ws, lay, x, w, wt
+
+
+# from 512 rows per SM on (75776 on 148 SMs) a warp of the sorting kernel takes four rows: experts begin and end inside them, tiles do, and the last warp has
+# fewer.  64 experts: CTA pairs, tiles of 256 and 208 rows; 1024 experts: single CTAs, tiles of 96.
+@pytest.mark.parametrize("T,E,k,d,f", [(20011, 64, 4, 64, 96), (20011, 1024, 4, 64, 32), (40003, 96, 2, 288, 64)])
+@pytest.mark.parametrize("flags", [0, B.MOE_FLAG_SPARSE_TOPK], ids=["plain", "sparse"])
+def test_expert_ffn_fp4_of_more_pairs_than_warps(T, E, k, d, f, flags):
+    assert T * k * 0.95 >= 512 * torch.cuda.get_device_properties(0).multi_processor_count
+    shape, ws, lay, x, w, wt = with_empty_experts(T, E, k, d, f, flags, T + E)
+    off = lay.expert_offsets[: E + 1].cpu().numpy()
+    assert (np.diff(off) == 0).sum() >= E // 5 and (off[1:] % 4 != 0).any() and (off[-1] < T * k) == (flags != 0)
+    check_ffn(shape, ws, lay, x, w, wt)
+
+
+# Every cluster (CTA) walks its pipeline round several times (six stages; single CTAs four) and comes to its accumulators a third time.  Pairs: GEMM-1 has 15 x 25
+# tiles of 9 stages, GEMM-2 19 x 9 of 13, for at most 74 clusters.  Single CTAs: 704 tiles of 6 stages, 384 of 6, for 148.
+@pytest.mark.parametrize("counts,d,f", [((1500, 700, 1300), 2080, 3104), ((0, 1029, 2100, 1), 3104, 1312), ((20, 19, 21, 23) * 16, 1312, 1312),
+                                        ((70, 0, 97, 33) * 16, 1056, 1312)], ids=["pairs", "pairs-2", "single", "single-2"])
+def test_expert_ffn_fp4_when_the_pipeline_comes_round(counts, d, f):
+    shape, ws, lay, x, xg, idx, w, wt = routed(counts, d=d, f=f, seed=len(counts) + d)
+    o = check_ffn(shape, ws, lay, xg, w, wt)
+    again = torch.full_like(o, 7.0)
+    B.moe_expert_ffn_fp4(shape, *rows_fp4(xg), lay, w, *quantised(wt), again, ws)
+    assert torch.equal(again, o)
+
+
+@pytest.mark.parametrize("T,E,k,G,d,f,score", [(3001, 16, 4, 4, 1056, 1312, 0), (1500, 64, 6, 8, 1312, 1056, 1), (9, 8, 2, 2, 4096, 2080, 0)])
+def test_layer_fp4_is_its_stages_at_size(T, E, k, G, d, f, score):
+    """The layer against its stages, bit for bit, eagerly and replayed from a graph with other tokens."""
+    cfg = H.synth.MoEConfig("fp4-size", T=T, d=d, f=f, E=E, k=k, G=G, score_fn=score, seed=T)
+    run = H.Run(cfg)
+    t, q = run.t, quantised([run.t["w1"], run.t["w3"], run.t["w2"]])
+    y = torch.zeros_like(run.y)
+
+    def stages():
+        run.route()
+        run.dispatch()
+        B.moe_expert_ffn_fp4(run.shape, *rows_fp4(run.xg), run.lay, run.w, *q, run.o, run.ws)
+        run.combine()
+        return run.y.clone()
+
+    want = stages()
+    B.moe_layer_fp4(run.shape, t["x"], t["w_gate"], t["bias"], *q, y, run.ws)
+    assert torch.equal(want, y)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.moe_layer_fp4(run.shape, t["x"], t["w_gate"], t["bias"], *q, y, run.ws)
+    t["x"].copy_(torch.randn(T, d, generator=torch.Generator(device="cuda").manual_seed(9), device="cuda"))
+    for _ in range(3):
+        y.zero_()
+        graph.replay()
+    torch.cuda.synchronize()
+    assert run.status()[0] == 0 and torch.equal(stages(), y)
+
+
+@pytest.mark.parametrize("d,f,E,k", [(512, 4096, 8, 2), (4096, 2048, 4, 1), (2048, 1024, 16, 2)])
+def test_fp4_workspace_of_a_batch_serves_smaller_ones(d, f, E, k):
+    """One workspace, allocated for the largest batch, for every smaller one, with the bits that a workspace of its own gives."""
+    g = torch.Generator(device="cuda").manual_seed(d)
+    wt = [torch.randn(E, K, N, generator=g, device="cuda").div(K ** 0.5).bfloat16() for K, N in ((d, f), (d, f), (f, d))]
+    q, wg = quantised(wt), torch.randn(d, E, generator=g, device="cuda") * 0.1
+    ws = B.alloc_workspace(B.MoEShape(600, d, f, E, k, 1, 0, 0))
+    ws[64:] = 0xEE
+    for T in (600, 97, 16, 3, 2, 1, 40, 600):
+        x = torch.randn(T, d, generator=g, device="cuda").bfloat16()
+        shape = B.MoEShape(T, d, f, E, k, 1, 0, 0)
+        y, want = torch.zeros_like(x), torch.zeros_like(x)
+        B.moe_layer_fp4(shape, x, wg, None, *q, y, ws)
+        B.moe_layer_fp4(shape, x, wg, None, *q, want, B.alloc_workspace(shape))
+        assert B.moe_status(ws)[0] == 0 and torch.equal(y, want), T

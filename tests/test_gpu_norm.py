@@ -329,3 +329,81 @@ def test_norm_backward_of_the_most_rows():
     assert not any(part.any().item() for part in dy.split(1 << 27))
     del s, dy, rstd
     torch.cuda.empty_cache()
+
+
+# ---- more rows than blocks ---------------------------------------------------------------------------------------------------
+def sms():
+    return torch.cuda.get_device_properties(0).multi_processor_count
+
+
+def varied(rows, cols, seed, std=1.0):
+    """Rows whose size differs from one to the next by up to 16 times: a sum that is taken from another row shows."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    size = torch.exp2(4 * torch.rand(rows, 1, generator=g, device="cuda"))
+    return (torch.randn(rows, cols, generator=g, device="cuda") * size * std).bfloat16()
+
+
+# as launched: at most 64 blocks per SM for 1025 to 4096 columns, 16 for the others; a block takes eight rows at once up to 1024 columns, else one
+@pytest.mark.parametrize("cols", [64, 640, 1536, 4096, 7168, 10000, 16384])
+@pytest.mark.parametrize("res,y,q", [(True, True, True), (False, True, False), (True, False, True), (False, True, True), (True, True, False)])
+def test_norm_when_blocks_take_several_rows(cols, res, y, q):
+    rows = 2 * sms() * (64 if 1024 < cols <= 4096 else 16) * (8 if cols <= 1024 else 1) + 5
+    x, r = varied(rows, cols, cols), varied(rows, cols, cols + 1) if res else None
+    w = 1 + 0.3 * torch.randn(cols, generator=torch.Generator(device="cuda").manual_seed(3), device="cuda")
+    out = forward(x, r, w, y, q)
+    wd = w.double()
+    for i in range(0, rows, 4096):
+        n = slice(i, min(rows, i + 4096))
+        s = x[n].double() + (r[n].double() if res else 0.0)
+        rstd = 1 / torch.sqrt(s.square().mean(1) + EPS)
+        ref = s * rstd[:, None] * wd
+        assert ((out["rstd"][n].double() - rstd).abs() <= CHAIN * U32 * rstd).all()
+        if res:
+            assert ((out["res"][n].double() - s).abs() <= (U16 + U32) * s.abs()).all()
+        err = (CHAIN + 4) * U32 * ref.abs()
+        if y:
+            assert ((out["y"][n].double() - ref).abs() <= U16 * ref.abs() + (1 + U16) * err).all()
+        if q:
+            sc = out["scale"][n].double()
+            top = ref.abs().amax(1) / 448
+            assert ((sc - top).abs() <= (CHAIN + 6) * U32 * top).all()
+            got = out["q"][n].view(torch.float8_e4m3fn).double() * sc[:, None]
+            assert ((got - ref).abs() <= (2.0 ** -4 + 2.0 ** -18) * ref.abs() + 2.0 ** -10 * sc[:, None]).all()
+
+
+# rows so that every stage of a block's ring (4 up to 512 and to 4096 columns, 3 to 1024 and to 8192, else 2) is filled at least three times
+@pytest.mark.parametrize("cols,rows", [(64, 60001), (640, 45003), (1504, 7500), (1536, 7500), (2880, 7500), (4096, 7500), (5000, 5500), (7168, 5500), (8192, 5500),
+                                       (12000, 3800), (16384, 3800)])
+@pytest.mark.parametrize("skip", [False, True])
+def test_norm_backward_when_the_ring_is_filled_again(cols, rows, skip):
+    n = sms()
+    assert rows > 3 * (4 if cols <= 512 or 1024 < cols <= 4096 else 3 if cols <= 8192 else 2) * 4 * n * (8 if cols <= 1024 else 1)
+    s, dy = varied(rows, cols, cols, 0.5), varied(rows, cols, cols + 1, 0.1)
+    k = varied(rows, cols, cols + 2, 0.1) if skip else None
+    w = 1 + 0.3 * torch.randn(cols, generator=torch.Generator(device="cuda").manual_seed(3), device="cuda")
+    rstd = torch.rsqrt(s.float().square().mean(1) + EPS)
+    dx, dw = backward(dy, s, w, rstd, k)
+    wd, dw_ref, dw_mag = w.double(), torch.zeros(cols, dtype=torch.float64, device="cuda"), torch.zeros(cols, dtype=torch.float64, device="cuda")
+    for i in range(0, rows, 4096):
+        m = slice(i, min(rows, i + 4096))
+        rv = rstd[m].double()[:, None]
+        xhat, a = s[m].double() * rv, dy[m].double()
+        g = a * wd
+        ref = rv * (g - xhat * (g * xhat).mean(1, keepdim=True)) + (k[m].double() if skip else 0.0)
+        mag = rv * (6 * g.abs() + xhat.abs() * (CHAIN + 6) * (g * xhat).abs().mean(1, keepdim=True))   # as in check_backward
+        err = U32 * (mag + ref.abs() + (k[m].double().abs() if skip else 0.0))
+        assert ((dx[m].double() - ref).abs() <= U16 * ref.abs() + (1 + U16) * err).all()
+        dw_ref += (a * xhat).sum(0)
+        dw_mag += (a * xhat).abs().sum(0)
+    # additions in a row: a block's rows (one block per SM at least), its eight warps, a warp's share of at most 592 blocks, the 32 lanes; 4 for a term
+    depth = -(-rows // n) + 8 + -(-592 // 32) + 5 + 4
+    assert ((dw.double() - dw_ref).abs() <= depth * U32 * dw_mag).all()
+    # over its inputs, and the same bits every time
+    again = torch.empty_like(dw)
+    ws = torch.empty(B.moe_rmsnorm_backward_workspace_bytes(rows, cols), dtype=torch.uint8, device="cuda")
+    for t in (dy, s, k):
+        if t is not None:
+            kept = t.clone()
+            B.moe_rmsnorm_backward(dy, s, w, rstd, t, again, ws, dres=k)
+            assert torch.equal(t, dx) and torch.equal(again, dw)
+            t.copy_(kept)
