@@ -143,7 +143,9 @@ ffn_fp4_kernel(const __grid_constant__ CUtensorMap map_wa, const __grid_constant
       next = tile_of(tile_at(0), 0);
       if (!GLU) f4_fetch_weights<F4_ROWS, 2>(p, next.row0, next.rows, turn, lane, rw);
     }
-    for (; tl < items && !*abort_flag; ++tl) {
+    // Looked at once, alike for all lanes: the wait's shuffle, which ends the loop after an abort, wants the whole warp.
+    const bool go = __all_sync(0xFFFFFFFFu, !*abort_flag);
+    for (; go && tl < items; ++tl) {
       t = next;
       if (!GLU) f4_keep_weights<F4_ROWS, 2>(rw, out_mem, lane);
       if (tl + 1 < items) {

@@ -146,7 +146,9 @@ ffn_fp4_pair_kernel(const __grid_constant__ CUtensorMap map_wa, const __grid_con
       next = tile_of(cluster_id, 0);
       if constexpr (!GLU) f4_fetch_weights<F4_PAIR_ROWS2, G::SHARES>(p, next.row0, next.rows, half, lane, rw);
     }
-    for (int w = cluster_id; w < total && !*abort_flag; w += num_clusters, ++tl) {
+    // Looked at once, alike for all lanes: the wait's shuffle, which ends the loop after an abort, wants the whole warp.
+    const bool go = __all_sync(0xFFFFFFFFu, !*abort_flag);
+    for (int w = cluster_id; go && w < total; w += num_clusters, ++tl) {
       t = next;
       if constexpr (!GLU) f4_keep_weights<F4_PAIR_ROWS2, G::SHARES>(rw, out_mem, lane);
       if (w + num_clusters < total) {

@@ -549,3 +549,20 @@ def test_fp4_workspace_of_a_batch_serves_smaller_ones(d, f, E, k):
         B.moe_layer_fp4(shape, x, wg, None, *q, y, ws)
         B.moe_layer_fp4(shape, x, wg, None, *q, want, B.alloc_workspace(shape))
         assert B.moe_status(ws)[0] == 0 and torch.equal(y, want), T
+
+
+@pytest.mark.parametrize("counts,d,f", [((3, 0, 20), 512, 4096), ((70, 33, 97), 288, 352), ((700, 300, 90), 288, 352)], ids=["shared", "single", "pairs"])
+def test_expert_ffn_fp4_on_an_aborted_workspace_ends(counts, d, f):
+    """The abort word of a wait that gave up makes the products skip their work; once it is reset the call gives the same bits as before."""
+    shape, ws, lay, x, xg, idx, w, wt = routed(counts, d=d, f=f, seed=d)
+    want = check_ffn(shape, ws, lay, xg, w, wt)
+    args = (shape, *rows_fp4(xg), lay, w, *quantised(wt))
+    o = torch.full_like(want, 7.0)
+    B.moe_selftest_wait_timeout(ws, 300_000)
+    B.moe_expert_ffn_fp4(*args, o, ws)
+    st = B.moe_status(ws)
+    assert st[0] == B.MOE_DEV_TIMEOUT and st[1] == 9 and st[4] == 1, st
+    assert (o == 7).all()
+    B.moe_status_reset(ws)
+    B.moe_expert_ffn_fp4(*args, o, ws)
+    assert B.moe_status(ws)[0] == 0 and torch.equal(o, want)

@@ -1,5 +1,6 @@
 """Refusals of the norm and the 4-bit operators, which come before any device is touched, and pins of their oracles."""
 import ctypes
+import re
 
 import numpy as np
 import pytest
@@ -247,3 +248,18 @@ def test_current_stream_with_and_without_the_direct_lookup(monkeypatch, has_look
         monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream", raising=False)
     assert B._stream(None) == (1003 if has_lookup else 4321)
     assert B._stream(Fake) == 4321
+
+
+def test_lanes_of_an_epilogue_warp_of_the_fp4_products_leave_together():
+    """The wait for a tile is a shuffle of the whole warp.  Were the abort word read lane by lane at the loop's head, some lanes could leave for the
+    block's barrier while the others stood at the shuffle; only the wait's own result, the same in every lane, ends the loop."""
+    from tests.test_boundary_cpu import enclosing_blocks, source
+    for fn in ("ffn_fp4.cu", "ffn_fp4_pair.cu"):
+        text = source(fn)
+        waits = [m.start() for m in re.finditer(r"\bmbar_wait_warp<", text)]
+        assert len(waits) == 1
+        head, start, end = [b for b in enclosing_blocks(text, waits[0]) if re.search(r"\b(for|while) \(", b[0])][-1]
+        assert "abort" not in head, f"{fn}: {head.strip()}"
+        leaves = re.findall(r"[^;{}]*[{;]?[^;{}]*\b(?:break|return|goto)\b", text[start:end])
+        assert len(leaves) == 1 and "timeout(1)" in leaves[0], leaves
+        assert re.search(r"const bool go = __all_sync\(0xFFFFFFFFu, !\*abort_flag\);", text[:start])
