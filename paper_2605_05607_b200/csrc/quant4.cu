@@ -66,7 +66,7 @@ __global__ void __launch_bounds__(256) dequantize_rows_fp4_kernel(const uint32_t
 
 // Weights [E, K, N] (N contiguous) -> codes [E, N, K / 2] and scale chunks [E, ceil(N / 128), 2 ceil(K / 256), 512].  A block takes 256 of K x 64
 // columns; a warp 32 of K, a lane two columns, whose 32 values it holds in registers.  Codes go through shared memory so that a column
-// leaves in 128-byte runs.  Bound by memory and by issue slots (61 % busy with conversions): 32 x 4096 x 1536 to codes and back 187 us, 175 with the
+// leaves in 128-byte runs.  Bound by memory and by issue slots (61 % busy with conversions): 32 x 4096 x 1536 to codes and back 187 us, 177 with the
 // maxima of both columns taken at once (5.8 TB/s).
 constexpr int WT_PITCH = 128 + 16;   // bytes per column in shared memory: neighbouring columns four banks apart
 __global__ void __launch_bounds__(256) quantize_weights_fp4_kernel(const uint32_t* __restrict__ w, uint4* __restrict__ wq,
