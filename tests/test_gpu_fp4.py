@@ -566,3 +566,67 @@ def test_expert_ffn_fp4_on_an_aborted_workspace_ends(counts, d, f):
     B.moe_status_reset(ws)
     B.moe_expert_ffn_fp4(*args, o, ws)
     assert B.moe_status(ws)[0] == 0 and torch.equal(o, want)
+
+
+# ---- offsets that pass 32 bits: the last part of a large call against a small call on that part alone --------------------------------
+def test_norm_and_rows_fp4_past_32_bits():
+    rows, cols, tail = (1 << 20) + 4099, 4096, 5000              # 4.3e9 elements
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.empty(rows, cols, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    w, y, rstd = torch.ones(cols, device="cuda"), torch.empty_like(x), torch.empty(rows, device="cuda")
+    B.moe_rmsnorm(x, w, 1e-6, y=y, rstd=rstd)
+    y2, rstd2 = torch.empty_like(x[-tail:]), torch.empty(tail, device="cuda")
+    B.moe_rmsnorm(x[-tail:], w, 1e-6, y=y2, rstd=rstd2)
+    assert torch.equal(y[-tail:], y2) and torch.equal(rstd[-tail:], rstd2)
+    dy = y                                                        # dx over dy
+    dx2, dw, ws = torch.empty_like(y2), torch.empty(cols, device="cuda"), torch.empty(B.moe_rmsnorm_backward_workspace_bytes(rows, cols), dtype=torch.uint8, device="cuda")
+    B.moe_rmsnorm_backward(y2, x[-tail:], w, rstd2, dx2, dw, ws)
+    B.moe_rmsnorm_backward(dy, x, w, rstd, dy, dw, ws)
+    assert torch.equal(dy[-tail:], dx2)
+    q, s = rows_fp4(x)
+    q2, s2 = rows_fp4(x[-tail:])
+    assert torch.equal(q[-tail:], q2) and torch.equal(s[-tail:], s2)
+    back, back2 = y, torch.empty_like(y2)
+    B.moe_dequantize_rows_fp4(q, s, back)
+    B.moe_dequantize_rows_fp4(q2, s2, back2)
+    assert torch.equal(back[-tail:], back2)
+    del x, y, dy, back, q
+    torch.cuda.empty_cache()
+
+
+def test_weights_fp4_past_32_bits():
+    E, K, N = 300, 7168, 2048                                     # 4.4e9 elements
+    w = torch.empty(E, K, N, dtype=torch.bfloat16, device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(2))
+    q, s = weights_fp4(w)
+    q2, s2 = weights_fp4(w[-2:])
+    assert torch.equal(q[-2:], q2) and torch.equal(s.view(E, -1)[-2:], s2.view(2, -1))
+    back2 = torch.empty_like(w[-2:])
+    B.moe_dequantize_weights_fp4(q2, s2, back2)
+    B.moe_dequantize_weights_fp4(q, s, w)
+    assert torch.equal(w[-2:], back2)
+    del w, q
+    torch.cuda.empty_cache()
+
+
+def test_expert_ffn_fp4_past_32_bits():
+    """1.1 M pairs of 4096 columns (o has 4.5e9 elements); the last tokens alone give the same rows."""
+    T, E, k, d, f, tail = 138000, 8, 8, 4096, 64, 3001
+    g = torch.Generator(device="cuda").manual_seed(3)
+    wt = [torch.randn(E, K, N, generator=g, device="cuda").div(K ** 0.5).bfloat16() for K, N in ((d, f), (d, f), (f, d))]
+    q = quantised(wt)
+    x = torch.empty(T, d, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    idx = torch.rand(T, E, generator=g, device="cuda").topk(k, dim=1).indices.int().contiguous()
+    w = torch.rand(T, k, generator=g, device="cuda") + 0.1
+    out = []
+    for n in (slice(0, T), slice(T - tail, T)):
+        xs, ids, ws_ = x[n].contiguous(), idx[n].contiguous(), w[n].contiguous()
+        shape = B.MoEShape(xs.shape[0], d, f, E, k, 1, 0, 0)
+        lay, ws = B.alloc_layout(shape), B.alloc_workspace(shape)
+        B.moe_dispatch(shape, None, ids, lay, None, ws)
+        o = torch.full((xs.shape[0] * k, d), 7.0, dtype=torch.bfloat16, device="cuda")
+        B.moe_expert_ffn_fp4(shape, *rows_fp4(xs), lay, ws_, *q, o, ws)
+        assert B.moe_status(ws)[0] == 0
+        out.append(o[lay.pair_row.view(-1, k)[-tail:].long().flatten()])
+        del o, ws
+    assert torch.equal(*out)
+    torch.cuda.empty_cache()
