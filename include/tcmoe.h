@@ -310,10 +310,10 @@ int moe_layer_fp8_host(const moe_shape_t* shape, const void* x_host, void* x_dev
  *   x, residual [rows, cols] bf16 (residual may be NULL: s = x);  weight [cols] bf16, or fp32 with weight_f32 != 0
  *   res_out     NULL, or bf16 out: s (needs residual);  y NULL, or bf16 out;  yq, scale both NULL, or E4M3 codes [rows, cols] and fp32 [rows]
  *   rstd        NULL, or fp32 [rows] out, for moe_rmsnorm_backward.  At least one of y and yq is not NULL.
- * res_out and y may be x or residual themselves (not both the same buffer).  The mean is taken in fp32: a row where it is not finite
- * (a NaN, an infinity, or values of about 1e19 and more, whose squares are not) gives NaN throughout, rstd, scale and codes included (res_out is s
- * all the same); so does, with eps = 0, a row whose mean vanishes.  Limits: cols % 8 == 0, cols <= 16384 (MOE_ERR_UNSUPPORTED_SHAPE); eps >= 0.  Alignment: 16 bytes, yq 8, scale
- * and rstd 4.  rows = 0 is accepted.  No workspace. */
+ * res_out and y may be x or residual themselves (not both the same buffer).  The sum of the squares is taken in fp32: a row where it is not
+ * finite (a NaN, an infinity, or a root mean square above 1.8e19 / sqrt(cols)) gives NaN throughout, rstd, scale and codes included (res_out is
+ * s all the same); so does, with eps = 0, a row whose squares vanish.  Limits: cols % 8 == 0, cols <= 16384 (MOE_ERR_UNSUPPORTED_SHAPE);
+ * eps >= 0.  Alignment: 16 bytes, yq 8, scale and rstd 4.  rows = 0 is accepted.  No workspace. */
 int moe_rmsnorm(const void* x, const void* residual, const void* weight, int32_t weight_f32, float eps, int64_t rows, int64_t cols,
                 void* res_out, void* y, void* yq, float* scale, float* rstd, void* stream);
 

@@ -1,7 +1,7 @@
 // Root-mean-square norm of the residual stream, the step in front of the layer, with the residual's addition, an E4M3 output with one
 // scale per row (the operand of the FP8 experts), and its backward pass.
 //     s = x + residual                    fp32; leaves as bf16 (the residual stream of the next block)
-//     rstd = 1 / sqrt(mean(s^2) + eps)     NaN, and with it the row, where the mean is not finite
+//     rstd = 1 / sqrt(mean(s^2) + eps)     NaN, and with it the row, where the sum is not finite
 //     y = (s * w) * rstd                  leaves as bf16 and / or as codes of y / scale, scale = max|y| / 448
 // Everything is computed from the fp32 sum: y and the codes are rounded once each, from fp32 (codes of the rounded y would round twice).
 // The product with w comes first so that one pass has both sums of the row: rounding is monotone, so max|y| is (max|s * w|) * rstd to the bit.
